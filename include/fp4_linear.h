@@ -54,6 +54,7 @@ extern "C" {
 #define FP4_ERR_ARG        (-7)   /* an argument has an unsupported value                    */
 #define FP4_ERR_CAPACITY   (-8)   /* sparse_cap is below fp4_sparse_capacity()               */
 #define FP4_ERR_STATIC_LIMIT (-9) /* input larger than the fixed scratch of a *_static call  */
+#define FP4_ERR_RANGE     (-10)   /* fp4_mx_*: a size or row stride is outside its range     */
 
 /* bits of the device status word (bit 0 is not used: the residual cannot outgrow a capacity the
  * host has accepted, see fp4_sparse_capacity) */
@@ -354,6 +355,134 @@ int64_t fp4_launch_count(fp4_ctx* ctx);
 #define FP4_STATIC_MAX_ROWS 65536
 int fp4_quantile_thresholds_static(void* stream, const void* x_bf16, int64_t rows, int64_t cols,
                                    double alpha, float* thresholds);
+
+/*
+ * Block-scaled ("microscaled") operands: fp4_mx_*.  Where the calls above scale a whole vector of the
+ * contraction, these scale blocks of it, so that an outlier costs its block's precision alone; nothing is
+ * clamped and no residual is kept.  (No counterpart in the paper, which scales vectors: Section 4.1.)
+ *
+ *   FP4_MX_E2M1   E2M1 nibbles, blocks of 32, scale 2^e (E8M0 byte e + 127): e is the least integer in
+ *                 [-127, 127] with amax <= 6 * 2^e, amax the block's largest magnitude (a block of zeros:
+ *                 -127); code = E2M1(x * 2^-e).  ("MXFP4".)
+ *   FP4_MX_NVFP4  E2M1 nibbles, blocks of 16, an E4M3 scale s each and a scale g of the whole tensor: g is
+ *                 the least power of two, 2^-100 at least, with the tensor's amax <= 6 * 448 * g;
+ *                 s = E4M3(amax / g / 6), code = E2M1(x / g / s), 0 where s is 0.  The tensor's amax is kept
+ *                 (`amax`), g follows from it.
+ *   FP4_MX_E4M3   E4M3 bytes, blocks of 32, scale 2^e with amax <= 448 * 2^e: the 8-bit form in which
+ *                 activations are kept for the backward pass.  fp4_mx_gemm does not take it.
+ * E2M1() and E4M3() round to the nearest value, ties to even, and saturate (which only a given amax that is
+ * too small can cause).  E2M1 codes of -0 are written as 0.  A block with an infinity or a NaN gets the
+ * scale NaN and codes 0, and the call raises FP4_DEV_NONFINITE; the other blocks are as specified.
+ *
+ * Sizes: any, zero included (nothing is launched for an empty tensor; a product over an empty contraction is
+ * 0); each at most 2^31 - 1, and at most 2^31 - 1 tiles of 128 x 128 of a tensor.  A matrix of the caller's
+ * (fp4_mx_matrix) is aligned to its element type and its rows may lie apart; rows that start on 16-byte
+ * boundaries are faster.  An output must not overlap an input.  The calls work on the context's device
+ * whichever is current, and launch no graphs; they share the workspace rule of the other calls.
+ */
+#define FP4_MX_E2M1   0
+#define FP4_MX_NVFP4  1
+#define FP4_MX_E4M3   2
+
+#define FP4_DTYPE_BF16 0
+#define FP4_DTYPE_FP16 1
+#define FP4_DTYPE_FP32 2
+
+/* A matrix: element (r, c) is at data[r * ld + c].  Pass NULL (or data == NULL) for one that is not wanted. */
+typedef struct fp4_mx_matrix {
+  void*   data;
+  int64_t ld;          /* row stride in elements, at least the number of columns (any for one row)  */
+  int32_t dtype;       /* FP4_DTYPE_*                                                              */
+  int32_t reserved;    /* 0                                                                        */
+} fp4_mx_matrix;
+
+/* A block-scaled tensor.  The caller owns the buffers, 16-byte aligned; a direction whose buffers are NULL
+ * is not made.  `codes` has one row per row of the tensor, blocks along the columns; `codes_t` one row per
+ * column, blocks along the rows (what a product contracts over must be what the blocks lie along).
+ *   row r, element c of codes: byte r * pitch + c / 2, even c in the low nibble (E4M3: r * pitch + c), with
+ *     pitch = fp4_mx_pitch(cols, format); elements behind the last are 0.
+ *   scale of row r, block b: byte (r / 128 * T + b / 4) * 512 + r % 32 * 16 + r % 128 / 32 * 4 + b % 4 with
+ *     T = ceil(cols / 128) (FP4_MX_NVFP4: twice that): the layout of the tensor cores' scale operand. Scales
+ *     behind the last row or block are 0.                                                              */
+typedef struct fp4_mx_tensor {
+  int64_t  rows, cols;
+  uint8_t* codes;      /* [rows x fp4_mx_pitch(cols)]                                                */
+  uint8_t* scales;     /* [fp4_mx_scale_bytes(rows, cols)]                                           */
+  uint8_t* codes_t;    /* [cols x fp4_mx_pitch(rows)]                                                */
+  uint8_t* scales_t;   /* [fp4_mx_scale_bytes(cols, rows)]                                           */
+  float*   amax;       /* [1] FP4_MX_NVFP4: largest magnitude of the tensor; else NULL               */
+  int32_t  format;     /* FP4_MX_*, set by the caller                                                */
+  int32_t  flags;      /* FP4_MX_AMAX_GIVEN: `amax` holds a value already (of earlier data, say): it is
+                          used and one pass over the tensor is saved; what exceeds it may saturate       */
+} fp4_mx_tensor;
+#define FP4_MX_AMAX_GIVEN 1
+
+/* Bytes of a row of `cols` codes and of the scales of rows x cols; -1 for arguments outside their range. */
+int64_t fp4_mx_pitch(int64_t cols, int format);
+int64_t fp4_mx_scale_bytes(int64_t rows, int64_t cols, int format);
+/* Workspace that fp4_mx_linear_bwd needs for these sizes (the other fp4_mx_* calls need none).           */
+size_t fp4_mx_workspace_bytes(int64_t M, int64_t K, int64_t N);
+
+/* Quantises x [out->rows x out->cols] along the directions whose buffers `out` has.  FP4_MX_NVFP4 reads x
+ * once more for its amax, unless that is given.                                                        */
+int fp4_mx_quantize(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, fp4_mx_tensor* out, int32_t* status);
+
+/* The values that the codes stand for, rounded once to out's type: [rows x cols] from `codes`, or with
+ * transposed != 0 [cols x rows] from `codes_t`.  (A value within its last rounding step of the type's
+ * largest may come out as infinity.)                                                                    */
+int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int transposed, const fp4_mx_matrix* out);
+
+/* out[i, j] = g_a g_b sum_c a[i, c] b[j, c], fp32 sums, rounded once; with FP4_MX_ACCUMULATE the former value
+ * of out is added before the rounding.  `a` is [I x C]: the tensor's rows (`codes`), or with FP4_MX_A_T its
+ * columns (`codes_t`, I = a->cols, C = a->rows); `b` [J x C] likewise.  Both have the same format, one of the
+ * two in E2M1.  Products of codes and scales are exact; the tensor cores add 64 of them at a time into the
+ * fp32 accumulator, rounding toward zero: the result is off by at most 2^-22 (C / 64 + 1) times the sum of
+ * the products' magnitudes.
+ * One row (a single token) up: with I <= 128 the rows of b spread over the GPU and clusters split the contraction. */
+#define FP4_MX_A_T        1
+#define FP4_MX_B_T        2
+#define FP4_MX_ACCUMULATE 4
+int fp4_mx_gemm(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* a, const fp4_mx_tensor* b, int flags,
+                const fp4_mx_matrix* out, int32_t* status);
+
+/*
+ * The linear layer Y = X W on block-scaled operands, X [M x K], W [K x N]:
+ *   forward    Y  = Q(X) Q(W)           blocks along K: saved_x->codes, saved_w->codes_t
+ *   backward   dX = Q(dY) Q(W)^T        blocks along N: saved_w->codes
+ *              dW = Q(X)^T Q(dY)        blocks along M: saved_x->codes_t
+ * with the straight-through gradient.  The forward quantises X into saved_x and W into saved_w, in every
+ * direction that has buffers: the ones for the backward pass may be left out (serving).  `reuse`: FP4_REUSE_X /
+ * FP4_REUSE_W -- that operand is there already (x or w may then be NULL).  saved_x and saved_w have the same
+ * format, FP4_MX_E2M1 or FP4_MX_NVFP4.  dx or dw may be NULL.  `flags` of the backward: FP4_MX_ACCUMULATE_DX /
+ * _DW add to what is there (a sum over consumers or micro-batches).
+ */
+#define FP4_REUSE_X FP4_REUSE_A
+#define FP4_MX_ACCUMULATE_DX 1
+#define FP4_MX_ACCUMULATE_DW 2
+int fp4_mx_linear_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, const fp4_mx_matrix* w, int64_t M,
+                      int64_t K, int64_t N, int reuse, const fp4_mx_matrix* y, fp4_mx_tensor* saved_x,
+                      fp4_mx_tensor* saved_w, int32_t* status);
+int fp4_mx_linear_bwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* dy, const fp4_mx_tensor* saved_x,
+                      const fp4_mx_tensor* saved_w, int64_t M, int64_t K, int64_t N, int flags,
+                      const fp4_mx_matrix* dx, const fp4_mx_matrix* dw, int32_t* status);
+
+/*
+ * SwiGLU between the gate / up and the down projection, with its inputs kept in 8 bits:
+ *   h = gate * sigmoid(gate) * up        [rows x cols], fp32 arithmetic, rounded once
+ * Any of: `h` as a matrix; `quantized`, h (rounded to the inputs' type) as the operand of the down projection,
+ * FP4_MX_E2M1, in the directions it has buffers for; ckpt_gate and ckpt_up (both or neither), FP4_MX_E4M3,
+ * `codes` and `scales`: what the backward pass needs instead of gate and up (8.25 bits a value).
+ * The backward reads them, g and u being the values they stand for, s = sigmoid(g):
+ *   d_up = dh * g * s,   d_gate = dh * u * (s + g * s * (1 - s))
+ * and makes h = g * s * u again on request (`h`, `quantized`: the weight gradient of the down projection needs
+ * its `codes_t`), so that h need not be kept either.  gate, up and h have one type; dh, dgate, dup and h too.
+ */
+int fp4_mx_swiglu_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* gate, const fp4_mx_matrix* up, int64_t rows,
+                      int64_t cols, const fp4_mx_matrix* h, fp4_mx_tensor* ckpt_gate, fp4_mx_tensor* ckpt_up,
+                      fp4_mx_tensor* quantized, int32_t* status);
+int fp4_mx_swiglu_bwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* dh, const fp4_mx_tensor* ckpt_gate,
+                      const fp4_mx_tensor* ckpt_up, int64_t rows, int64_t cols, const fp4_mx_matrix* dgate,
+                      const fp4_mx_matrix* dup, const fp4_mx_matrix* h, fp4_mx_tensor* quantized, int32_t* status);
 
 #ifdef __cplusplus
 }

@@ -11,4 +11,8 @@ from .binding import (  # noqa: F401
     Context, Fp4Error, QTensor, fp4_gemm, fp4_linear_bwd, fp4_linear_fwd, fp4_linear_step_host, fp4_quantile_thresholds_static, fp4_quantize, fp4_l2_read_probe, load_library,
     tail_capacity, KERNEL_CLASSES,
 )
+from .mx import (  # noqa: F401
+    FP4_DTYPE_BF16, FP4_DTYPE_FP16, FP4_DTYPE_FP32, FP4_MX_E2M1, FP4_MX_E4M3, FP4_MX_NVFP4, MXTensor, SwigluCheckpoint,
+    fp4_mx_dequantize, fp4_mx_gemm, fp4_mx_linear_bwd, fp4_mx_linear_fwd, fp4_mx_quantize, fp4_mx_swiglu_bwd, fp4_mx_swiglu_fwd,
+)
 from . import workloads  # noqa: F401

@@ -32,7 +32,8 @@ EXPORTS = ("fp4_create", "fp4_destroy", "fp4_workspace_bytes", "fp4_status_strin
            "fp4_gemm", "fp4_linear_fwd", "fp4_linear_bwd", "fp4_step_host_workspace_bytes",
            "fp4_linear_step_host", "fp4_profile_enable", "fp4_profile_reset", "fp4_profile_read",
            "fp4_launch_count", "fp4_quantile_thresholds_static", "fp4_set_overlap", "fp4_l2_read_probe", "fp4_debug_set", "fp4_sparse_capacity",
-           "fp4_set_quantile_mode")
+           "fp4_set_quantile_mode", "fp4_mx_pitch", "fp4_mx_scale_bytes", "fp4_mx_workspace_bytes", "fp4_mx_quantize",
+           "fp4_mx_dequantize", "fp4_mx_gemm", "fp4_mx_linear_fwd", "fp4_mx_linear_bwd", "fp4_mx_swiglu_fwd", "fp4_mx_swiglu_bwd")
 FP4_STATIC_MAX_ROWS = 65536
 FP4_QUANTILE_SIGNED = 0
 FP4_QUANTILE_ABS = 1
@@ -110,6 +111,8 @@ def load_library(path: str | None = None) -> C.CDLL:
     lib.fp4_launch_count.restype = C.c_int64
     lib.fp4_quantile_thresholds_static.argtypes = [vp, vp, i64, i64, C.c_double, vp]
     lib.fp4_quantile_thresholds_static.restype = C.c_int
+    from .mx import declare
+    declare(lib)
     if path == LIB_PATH:
         _lib = lib
     return lib
@@ -150,6 +153,11 @@ class Context:
     @classmethod
     def for_shape(cls, M: int, K: int, N: int, device: int = 0):
         return cls(device, int(load_library().fp4_workspace_bytes(M, K, N)))
+
+    @classmethod
+    def for_mx(cls, M: int, K: int, N: int, device: int = 0):
+        """A context whose workspace serves the block-scaled calls (fp4_mx_*) of these sizes."""
+        return cls(device, int(load_library().fp4_mx_workspace_bytes(M, K, N)))
 
     def close(self):
         if self.handle:

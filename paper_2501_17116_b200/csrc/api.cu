@@ -115,6 +115,7 @@ const char* fp4_status_string(int code) {
     case FP4_ERR_ARG: return "an argument has an unsupported value";
     case FP4_ERR_CAPACITY: return "sparse_cap is below fp4_sparse_capacity()";
     case FP4_ERR_STATIC_LIMIT: return "input exceeds the fixed scratch of the allocation-free entry point";
+    case FP4_ERR_RANGE: return "a size or row stride is outside its range";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,66 @@
+// Block-scaled ("microscaled") operands: layout, scale arithmetic and internal launchers (the public ABI is
+// include/fp4_linear.h).  Internal.
+//
+// An operand of `rows` vectors of `cols` elements, scaled in blocks along `cols`:
+//   codes   [rows x pitch], pitch = ceil(cols / 128) * 64 bytes of E2M1 nibbles (even element low) or * 128 of
+//           E4M3 bytes; what lies behind `cols` is zero
+//   scales  one byte per block, in tiles of 128 rows x 4 blocks (512 bytes): row r, block b at
+//             tile (r / 128) * T + b / 4, byte (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4,
+//           T = ceil(cols / 128) (E2M1 in blocks of 16: twice that).  It is the order in which tcgen05.cp
+//           (32x128b.warpx4) hands the scales of 128 rows to tensor memory: four columns, four lane quarters alike.
+//           Bytes that stand for no block are zero.
+#pragma once
+
+#include "common.cuh"
+
+constexpr int MX_TILE = 128;
+
+__host__ __device__ constexpr bool mx_known(int format) { return format >= FP4_MX_E2M1 && format <= FP4_MX_E4M3; }
+__host__ __device__ constexpr int mx_block(int format) { return format == FP4_MX_NVFP4 ? 16 : 32; }
+__host__ __device__ constexpr int64_t mx_tiles(int64_t n) { return (n + MX_TILE - 1) / MX_TILE; }
+__host__ __device__ constexpr int64_t mx_pitch(int64_t cols, int format) {
+  return mx_tiles(cols) * (format == FP4_MX_E4M3 ? 128 : 64);
+}
+__host__ __device__ constexpr int64_t mx_scale_tiles(int64_t cols, int format) {
+  return mx_tiles(cols) * (format == FP4_MX_NVFP4 ? 2 : 1);
+}
+__host__ __device__ constexpr int64_t mx_scale_bytes(int64_t rows, int64_t cols, int format) {
+  return mx_tiles(rows) * mx_scale_tiles(cols, format) * 512;
+}
+
+// Scale of an NVFP4 tensor: the least 2^k, k >= -100, with amax <= 6 * 448 * 2^k (2688 = 1.3125 * 2^11; the sum carries into
+// the exponent where the mantissa is larger).  A power of two, so that dividing by it is exact: whether a value of a 16-bit
+// type lies on a tie of its format is then decided without a rounding.
+__host__ __device__ inline int mx_tensor_exponent(uint32_t amax_bits) {
+  const int k = int(((amax_bits & 0x7FFFFFFFu) + (0x7FFFFFu - 0x280000u)) >> 23) - 127 - 11;
+  return k < -100 ? -100 : k;
+}
+
+struct MxMatrix {               // a matrix of the caller's: rows of `ld` elements
+  const void* p;
+  int64_t ld;
+};
+
+int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, MxMatrix x, int dtype, const fp4_mx_tensor& q, int32_t* status);
+int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes, const uint8_t* scales, const float* amax,
+                         int64_t rows, int64_t cols, int format, void* out, int64_t ld, int dtype);
+// `h` may have no pointer; `q` (may be null): E2M1 in blocks of 32.
+int launch_mx_swiglu_fwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix gate, MxMatrix up, int64_t rows, int64_t cols, int dtype,
+                         MxMatrix h, const fp4_mx_tensor* ckpt_gate, const fp4_mx_tensor* ckpt_up, const fp4_mx_tensor* q,
+                         int32_t* status);
+int launch_mx_swiglu_bwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix dh, const fp4_mx_tensor& gate, const fp4_mx_tensor& up,
+                         int64_t rows, int64_t cols, int dtype, MxMatrix dgate, MxMatrix dup, MxMatrix h,
+                         const fp4_mx_tensor* q, int32_t* status);
+
+// out[i, j] (+)= g_a g_b sum_c a[i, c] b[j, c]
+struct MxGemm {
+  const uint8_t *a, *a_scales, *b, *b_scales;
+  const float *a_amax, *b_amax;      // NVFP4: the operands' amax
+  int64_t I, J, C;
+  int format;
+  void* out;
+  int64_t ld;
+  int dtype;
+  bool accumulate;
+};
+int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* status);
