@@ -11,6 +11,8 @@
 //           Bytes that stand for no block are zero.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 
 constexpr int MX_TILE = 128;
@@ -34,6 +36,17 @@ __host__ __device__ constexpr int64_t mx_scale_bytes(int64_t rows, int64_t cols,
 __host__ __device__ inline int mx_tensor_exponent(uint32_t amax_bits) {
   const int k = int(((amax_bits & 0x7FFFFFFFu) + (0x7FFFFFu - 0x280000u)) >> 23) - 127 - 11;
   return k < -100 ? -100 : k;
+}
+
+// More than 48 KB of shared memory for a kernel: asked for once per kernel and device (the call takes half a microsecond).
+template <auto KERNEL>
+cudaError_t mx_allow_smem(int device, int bytes) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 struct MxMatrix {               // a matrix of the caller's: rows of `ld` elements

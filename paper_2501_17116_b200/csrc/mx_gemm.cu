@@ -20,6 +20,8 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "mx.cuh"
 #include "tc_ptx.cuh"
 
@@ -30,8 +32,9 @@ constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int A_BYTES = BM * 128;                 // codes of a k-block of 128 rows
 constexpr int TMEM_COLS = 512;
-constexpr int BN_MAX = 192;                       // 2 x 192 accumulator columns leave room for the scales; a multiple of 64, so that
-                                                  // a tile's columns begin at a half of a scale tile at least
+// Widths are multiples of 64: a tile's columns then begin at a half of a scale tile at least.  Tensor memory holds 192 columns twice
+// beside the scales; of 256 columns the second accumulator stage shares its first columns with the first stage's last.
+constexpr int BN_TWICE = 192, BN_MAX = 256;
 constexpr int MAX_STAGES = 6;
 constexpr int STAGE_OUT = 4096;                   // of an epilogue warp
 constexpr int MISC_BYTES = 256;
@@ -39,8 +42,11 @@ constexpr int MOST_SMEM = 227 * 1024;
 
 __host__ __device__ constexpr int scale_tiles(int fmt) { return fmt == FP4_MX_NVFP4 ? 4 : 2; }      // of a k-block
 __host__ __device__ constexpr int scale_bytes(int fmt) { return scale_tiles(fmt) * 512; }           // of 128 rows
-// Tensor memory: accumulators at 0 and BN_MAX, then two sets of scales (k-blocks alternate): A's, 4 columns a tile, and B's, 8.
+// Tensor memory: accumulators at 0 and acc_offset, then the scales: A's, 4 columns a tile, and B's, 8; two sets of them, which
+// k-blocks take in turn, where there is room.
 __host__ __device__ constexpr int sf_cols(int fmt) { return scale_tiles(fmt) * 12; }
+__host__ __device__ constexpr int sf_offset_wide(int fmt) { return fmt == FP4_MX_NVFP4 ? 448 : 480; }
+__host__ __device__ constexpr int acc_offset(int fmt, bool wide) { return wide ? sf_offset_wide(fmt) - BN_MAX : BN_TWICE; }
 
 constexpr uint32_t idesc_mx(int fmt, int m, int n) {
   return (1u << 7) | (1u << 10) | (uint32_t(n >> 3) << 17) | (fmt == FP4_MX_NVFP4 ? 0u : 1u << 23) | (uint32_t(m >> 4) << 24);
@@ -74,6 +80,12 @@ __device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
 // No swizzle: groups of eight 16-byte rows, 128 bytes apart.
 __device__ __forceinline__ uint64_t scale_desc(uint32_t smem_addr) {
   return uint64_t((smem_addr & 0x3FFFFu) >> 4) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
+}
+
+// Arrives on a barrier of the pair's even CTA.  What it says (these accumulators have been read) is no data in memory, and the arrival
+// needs no release at cluster scope, which takes 1200 cycles more, in the path from one tile to the next.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // One k-block: its scales to tensor memory, then four MMAs.  `sfb_cols`: columns of B's scales per tile; `sfb_shift`: 2 where the
@@ -116,23 +128,12 @@ template <> struct OutOf<FP4_DTYPE_FP32> {
   __device__ static float get(float v) { return v; }
   __device__ static float put(float v) { return v; }
 };
-template <int DT>
-__device__ __forceinline__ void put_one(void* out, int64_t at, float v, bool accumulate) {
-  typename OutOf<DT>::type* p = static_cast<typename OutOf<DT>::type*>(out) + at;
-  *p = OutOf<DT>::put(accumulate ? v + OutOf<DT>::get(*p) : v);
-}
-__device__ __forceinline__ void put_any(void* out, int64_t at, float v, bool accumulate, int dtype) {
-  if (dtype == FP4_DTYPE_BF16) put_one<FP4_DTYPE_BF16>(out, at, v, accumulate);
-  else if (dtype == FP4_DTYPE_FP16) put_one<FP4_DTYPE_FP16>(out, at, v, accumulate);
-  else put_one<FP4_DTYPE_FP32>(out, at, v, accumulate);
-}
-
 struct OutArgs {
   void* p;
   int64_t ld;
   int I, J, dtype;
   bool accumulate;
-  bool bulk;                   // rows on 16-byte boundaries and nothing to add to: bulk stores
+  bool bulk;                   // rows begin and end on 16-byte boundaries: bulk stores
 };
 // The tensors' powers of two (1 without them).
 struct Powers {
@@ -147,61 +148,153 @@ __device__ __forceinline__ float2 tensor_scales(const Powers& p) {
   return s;
 }
 
-// 32 rows x 32 columns (the last chunk: fewer) of a warp, row `lane` in y.
-__device__ __forceinline__ void store_chunk(const float (&y)[32], uint8_t* stage, const OutArgs& o, const CUtensorMap* map, int row0,
-                                            int col0, int lane, uint32_t& seq) {
-  if (o.bulk) {
-    // boxes of 32 rows x 64 bytes through two 2 KB buffers in turn; with the 64-byte swizzle 16-byte slot s of row r sits at
-    // s ^ ((r >> 1) & 3), so the rows' writes touch every bank once
-    const int fx = (lane >> 1) & 3;
-    const int boxes = o.dtype == FP4_DTYPE_FP32 ? 2 : 1;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if (u >= boxes || (u && col0 + 16 >= o.J)) break;
-      uint8_t* buf = stage + (seq & 1u) * 2048;
-      ++seq;
-      if (elect_one()) tma_store_wait_read_1();
-      __syncwarp();
-      uint8_t* my_row = buf + lane * 64;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint4 q;
-        if (o.dtype == FP4_DTYPE_FP32) {
-          const float* v = y + 16 * u + 4 * j;
-          q = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        } else {
-          uint32_t w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (o.dtype == FP4_DTYPE_BF16) {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(y[8 * j + 2 * i], y[8 * j + 2 * i + 1]);
-              w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            } else {
-              const __half2 h = __floats2half2_rn(y[8 * j + 2 * i], y[8 * j + 2 * i + 1]);
-              w[i] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-          }
-          q = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        *reinterpret_cast<uint4*>(my_row + ((j ^ fx) * 16)) = q;
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (elect_one()) tma_store_2d(map, buf, col0 + 16 * u, row0);
-    }
+// 32 rows x 32 columns (the last chunk: fewer) of a warp, row `lane` in y.  Three ways out:
+//   BULK      boxes of 32 rows x 64 bytes through shared memory to the copy engine
+//   BULK_ADD  the same, what is there added first: every lane reads its row's 64 (fp32: 128) bytes
+//   ANY       any alignment: through shared memory, so that a row's values lie in a row of lanes
+enum Way { BULK = 0, BULK_ADD = 1, ANY = 2 };
+template <int DT>
+__device__ __forceinline__ uint32_t two_values(float a, float b) {
+  if constexpr (DT == FP4_DTYPE_BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
   } else {
-    // any alignment, or results to be added to what is there: through shared memory, so that a row's values lie in a row of lanes
-    float* buf = reinterpret_cast<float*>(stage);
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<float4*>(buf + lane * 32 + ((j ^ (lane & 7)) * 4)) = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
-    __syncwarp();
-    const int rows = min(32, o.I - row0);
-    if (col0 + lane < o.J)
-      for (int r = 0; r < rows; ++r)
-        put_any(o.p, int64_t(row0 + r) * o.ld + col0 + lane, buf[r * 32 + (((lane >> 2) ^ (r & 7)) * 4) + (lane & 3)], o.accumulate, o.dtype);
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
   }
+}
+template <int DT>
+__device__ __forceinline__ float2 two_floats(uint32_t w) {
+  if constexpr (DT == FP4_DTYPE_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <int DT>
+struct Old {                   // what is there of a lane's row, as it lies in memory
+  uint4 q[DT == FP4_DTYPE_FP32 ? 8 : 4];
+};
+template <int DT>
+__device__ __forceinline__ void load_old(Old<DT>& old, const OutArgs& o, int row, int col0) {
+  constexpr int PER = DT == FP4_DTYPE_FP32 ? 4 : 8;      // values in 16 bytes; a row has whole ones (OutArgs::bulk)
+  const typename OutOf<DT>::type* p = static_cast<const typename OutOf<DT>::type*>(o.p) + int64_t(row) * o.ld + col0;
+#pragma unroll
+  for (int i = 0; i < 32 / PER; ++i) {
+    old.q[i] = make_uint4(0, 0, 0, 0);
+    if (row < o.I && col0 + i * PER < o.J) old.q[i] = *reinterpret_cast<const uint4*>(p + i * PER);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void add_old(float (&y)[32], const Old<DT>& old) {
+#pragma unroll
+  for (int i = 0; i < (DT == FP4_DTYPE_FP32 ? 8 : 4); ++i) {
+    const uint32_t w[4] = {old.q[i].x, old.q[i].y, old.q[i].z, old.q[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (DT == FP4_DTYPE_FP32) {
+        y[4 * i + k] += __uint_as_float(w[k]);
+      } else {
+        const float2 f = two_floats<DT>(w[k]);
+        y[8 * i + 2 * k] += f.x;
+        y[8 * i + 2 * k + 1] += f.y;
+      }
+    }
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_bulk(const float (&y)[32], uint8_t* stage, const OutArgs& o, const CUtensorMap* map, int row0,
+                                           int col0, int lane, uint32_t& seq) {
+  // two 2 KB buffers in turn; with the 64-byte swizzle 16-byte slot s of row r sits at s ^ ((r >> 1) & 3), so the rows' writes touch
+  // every bank once
+  const int fx = (lane >> 1) & 3;
+#pragma unroll
+  for (int u = 0; u < (DT == FP4_DTYPE_FP32 ? 2 : 1); ++u) {
+    if (u && col0 + 16 >= o.J) break;
+    uint8_t* buf = stage + (seq & 1u) * 2048;
+    ++seq;
+    if (elect_one()) tma_store_wait_read_1();
+    __syncwarp();
+    uint8_t* my_row = buf + lane * 64;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint4 q;
+      if constexpr (DT == FP4_DTYPE_FP32) {
+        const float* v = y + 16 * u + 4 * j;
+        q = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      } else {
+        const float* v = y + 8 * j;
+        q = make_uint4(two_values<DT>(v[0], v[1]), two_values<DT>(v[2], v[3]), two_values<DT>(v[4], v[5]), two_values<DT>(v[6], v[7]));
+      }
+      *reinterpret_cast<uint4*>(my_row + ((j ^ fx) * 16)) = q;
+    }
+    fence_async_smem();
+    __syncwarp();
+    if (elect_one()) tma_store_2d(map, buf, col0 + 16 * u, row0);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_any(const float (&y)[32], uint8_t* stage, const OutArgs& o, int row0, int col0, int lane) {
+  typedef typename OutOf<DT>::type T;
+  float* buf = reinterpret_cast<float*>(stage);
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<float4*>(buf + lane * 32 + ((j ^ (lane & 7)) * 4)) = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+  __syncwarp();
+  const int rows = min(32, o.I - row0);
+  if (col0 + lane >= o.J) return;
+  T* p = static_cast<T*>(o.p) + int64_t(row0) * o.ld + col0 + lane;
+  constexpr int AT_ONCE = 8;                               // rows whose old values are on their way together
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
+    float v[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int r = r0 + i;
+      v[i] = buf[r * 32 + (((lane >> 2) ^ (r & 7)) * 4) + (lane & 3)];
+      if (o.accumulate && r < rows) v[i] += OutOf<DT>::get(p[int64_t(r) * o.ld]);
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (r0 + i < rows) p[int64_t(r0 + i) * o.ld] = OutOf<DT>::put(v[i]);
+  }
+}
+
+// One tile's accumulators (args.bn columns from `t_base` on) for one warp: the two warps of a lane quarter take chunks of 32 columns
+// in turn.  `free_bar`: barrier that says the accumulators may be overwritten, 0 where that is not this lane's to say.
+template <int DT, int WAY>
+__device__ __forceinline__ uint32_t store_tile(uint32_t t_base, int bn, bool wide, bool first_stage, int group, int row0, int n0, const OutArgs& o,
+                                            const CUtensorMap* map, uint8_t* stage, int lane, uint32_t seq, float2 scales,
+                                            uint32_t free_bar) {
+  const int n_valid = min(bn, o.J - n0), chunks = bn / 32;
+#pragma unroll 1
+  for (int i = group; i < chunks; i += 2) {
+    // the columns that the stages share (wide: the first stage's last ones, the second's first) go ahead of the others
+    const int c = 32 * (wide && first_stage ? chunks - 1 - i : i);
+    const bool some = c < n_valid && row0 < o.I;
+    float y[32];
+    Old<DT> old;
+    constexpr bool EARLY = WAY == BULK_ADD && DT != FP4_DTYPE_FP32;      // (fp32: the accumulators need the registers)
+    if (EARLY && some) load_old<DT>(old, o, row0 + lane, n0 + c);
+    if (some) {
+      uint32_t v[32];
+      tmem_ld_32x32(t_base + uint32_t(c), v);
+      tmem_ld_wait(v);
+#pragma unroll
+      for (int k = 0; k < 32; ++k) y[k] = __uint_as_float(v[k]) * scales.x * scales.y;
+    }
+    if (wide ? i == group : i + 2 >= chunks) {
+      tc_fence_before();
+      __syncwarp();
+      if (free_bar) mbar_arrive_remote(free_bar);
+    }
+    if (!some) continue;
+    if (WAY == BULK_ADD) {
+      if (!EARLY) load_old<DT>(old, o, row0 + lane, n0 + c);
+      add_old<DT>(y, old);
+    }
+    if (WAY == ANY) store_any<DT>(y, stage, o, row0, n0 + c, lane);
+    else store_bulk<DT>(y, stage, o, map, row0, n0 + c, lane, seq);
+  }
+  return seq;
 }
 
 struct GemmArgs {
@@ -216,7 +309,7 @@ struct GemmArgs {
 };
 constexpr int FIXED_SMEM = 1024 + MISC_BYTES + EPI_WARPS * STAGE_OUT;
 
-template <int FMT, bool PAIR>
+template <int FMT, bool PAIR, int DT>
 __global__ void __launch_bounds__(THREADS, 1)
 mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
@@ -241,6 +334,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   const int num_tiles = args.num_m_blocks * args.num_n_blocks;
   const int rank = PAIR ? int(cluster_ctarank()) : 0;
   const int worker = int(blockIdx.x) / CTAS, workers = int(gridDim.x) / CTAS;
+  const bool wide = args.bn > BN_TWICE;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -256,6 +350,20 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
+  const uint32_t full0 = PAIR ? cluster_address(full_bar, 0) : smem_u32(full_bar);      // (a pair's copies complete on the even CTA's)
+  const auto request = [&](int m_blk, int n0, int kb, int stage) {
+    uint8_t* p = smem + stage * STAGE_BYTES;
+    const uint32_t bar = full0 + 8 * stage;
+    if (rank == 0) mbar_arrive_expect_tx(&full_bar[stage], CTAS * args.tx_bytes);
+    tma_load_2d_group<CTAS>(p, &map_a, bar, kb * 128, m_blk * BM);
+    tma_load_2d_group<CTAS>(p + A_BYTES, &map_b, bar, kb * 128, n0 + rank * (args.bn / CTAS));
+    tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes, &map_sa, bar, kb * (scale_bytes(FMT) / 8), m_blk);
+    tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes + scale_bytes(FMT), &map_sb, bar, kb * (scale_bytes(FMT) / 8), n0 / 128);
+  };
+  // Single CTAs: the stages are empty and the barriers this thread's own work, so the first tile's first k-blocks travel while tensor
+  // memory is allocated.  (A pair's barriers have to be known to exist first.)
+  if (!PAIR && threadIdx.x == 0 && worker < num_tiles)
+    for (int s = 0; s < STAGES && s < args.num_k_blocks; ++s) request(worker % args.num_m_blocks, worker / args.num_m_blocks * args.bn, s, s);
   if (warp == 1) tmem_alloc<CTAS>(tmem_slot, TMEM_COLS);
   tc_fence_before();
   __syncthreads();
@@ -269,20 +377,14 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       int stage = 0;
       uint32_t phase = 0, fills = 0;
       bool ok = true;
-      const uint32_t full0 = PAIR ? cluster_address(full_bar, 0) : smem_u32(full_bar);
       for (int t = worker; t < num_tiles && ok; t += workers) {
         const int m_blk = CTAS * (t % args.num_m_blocks) + rank, n0 = (t / args.num_m_blocks) * args.bn;
-        const int b_row = n0 + rank * (args.bn / CTAS);
         for (int kb = 0; kb < args.num_k_blocks; ++kb) {
-          ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
-          if (!ok) break;
-          uint8_t* p = smem + stage * STAGE_BYTES;
-          const uint32_t bar = full0 + 8 * stage;
-          if (rank == 0) mbar_arrive_expect_tx(&full_bar[stage], CTAS * args.tx_bytes);
-          tma_load_2d_group<CTAS>(p, &map_a, bar, kb * 128, m_blk * BM);
-          tma_load_2d_group<CTAS>(p + A_BYTES, &map_b, bar, kb * 128, b_row);
-          tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes, &map_sa, bar, kb * (scale_bytes(FMT) / 8), m_blk);
-          tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes + scale_bytes(FMT), &map_sb, bar, kb * (scale_bytes(FMT) / 8), n0 / 128);
+          if (PAIR || t != worker || kb >= STAGES) {            // (those are on their way)
+            ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
+            if (!ok) break;
+            request(m_blk, n0, kb, stage);
+          }
           ++fills;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
@@ -312,29 +414,31 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer ---------
     if (rank == 0 && elect_one()) {
-      int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0, sf = 0;
+      int stage = 0, n = 0;                     // n: tiles so far
+      uint32_t phase = 0, sf = 0;
       bool ok = true;
-      for (int t = worker; t < num_tiles && ok; t += workers) {
-        ok = mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
+      for (int t = worker; t < num_tiles && ok; t += workers, ++n) {
+        const int acc = n & 1;
+        const uint32_t d_tmem = tmem_base + uint32_t(acc * acc_offset(FMT, wide));
+        const int shift = (t / args.num_m_blocks) * args.bn % 128 ? 2 : 0;
+        // A stage is free when the tile before the last has left it.  Wide: when the last has left the columns that both stages have.
+        const int back = wide ? 1 : 2;
+        ok = n < back || mbar_wait(&acc_empty[(n - back) & 1], uint32_t((n - back) >> 1) & 1u, abort_flag, args.status, args.wait_limit_ns);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t d_tmem = tmem_base + uint32_t(acc * BN_MAX);
-        const int shift = (t / args.num_m_blocks) * args.bn % 128 ? 2 : 0;
         for (int kb = 0; kb < args.num_k_blocks; ++kb) {
           ok = mbar_wait(&full_bar[stage], phase, abort_flag, args.status, args.wait_limit_ns);
           if (!ok) break;
           tc_fence_after();
           const uint32_t p = smem_u32(smem + stage * STAGE_BYTES);
           issue_k_block<FMT, CTAS>(p, p + A_BYTES, p + A_BYTES + b_bytes, p + A_BYTES + b_bytes + scale_bytes(FMT), args.b_tiles, d_tmem,
-                                   tmem_base + 2 * BN_MAX + sf * sf_cols(FMT), shift, args.idesc, kb == 0);
+                                   tmem_base + (wide ? sf_offset_wide(FMT) : 2 * BN_TWICE + sf * sf_cols(FMT)), shift, args.idesc, kb == 0);
           sf ^= 1u;
           tc_commit_all<CTAS>(&empty_bar[stage]);
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
         if (!ok) break;
         tc_commit_all<CTAS>(&acc_full[acc]);
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
       // All that this thread issued must have retired before tensor memory is freed.
       tc_commit<CTAS>(final_bar);
@@ -354,28 +458,21 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     uint32_t acc_phase = 0, seq = 0;
     const uint32_t acc_empty0 = PAIR ? cluster_address(acc_empty, 0) : smem_u32(acc_empty);
     const float2 scales = tensor_scales(args.powers);
+    const int way = !args.out.bulk ? ANY : args.out.accumulate ? BULK_ADD : BULK;
     for (int t = worker; t < num_tiles; t += workers) {
       const int m_blk = CTAS * (t % args.num_m_blocks) + rank, n0 = (t / args.num_m_blocks) * args.bn;
-      const bool ok = mbar_wait(&acc_full[acc], acc_phase, abort_flag, args.status, args.wait_limit_ns);
-      if (epilogue_bar_any(!ok, 32 * EPI_WARPS)) break;
+      if (!__all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, args.status, args.wait_limit_ns))) break;
       tc_fence_after();
-      const uint32_t t_base = tmem_base + (uint32_t(quarter * 32) << 16) + uint32_t(acc * BN_MAX);
-      const int row0 = m_blk * BM + quarter * 32, n_valid = min(args.bn, args.out.J - n0);
-      if (row0 < args.out.I)
-        for (int c = 32 * group; c < n_valid; c += 64) {
-          uint32_t v[32];
-          tmem_ld_32x32(t_base + uint32_t(c), v);
-          tmem_ld_wait(v);
-          float y[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) y[i] = __uint_as_float(v[i]) * scales.x * scales.y;
-          store_chunk(y, stage, args.out, &map_out, row0, n0 + c, lane, seq);
-        }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) mbar_arrive_cluster(acc_empty0 + 8 * acc); else mbar_arrive(&acc_empty[acc]);
-      }
+      const uint32_t t_base = tmem_base + (uint32_t(quarter * 32) << 16) + uint32_t(acc * acc_offset(FMT, wide));
+      const int row0 = m_blk * BM + quarter * 32;
+      const uint32_t free_bar = lane == 0 ? acc_empty0 + 8 * acc : 0u;
+      const auto store = [&](auto the_way) {
+        seq = store_tile<DT, decltype(the_way)::value>(t_base, args.bn, wide, acc == 0, group, row0, n0, args.out, &map_out, stage, lane, seq,
+                                                       scales, free_bar);
+      };
+      if (way == BULK) store(std::integral_constant<int, BULK>());
+      else if (way == BULK_ADD) store(std::integral_constant<int, BULK_ADD>());
+      else store(std::integral_constant<int, ANY>());
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (elect_one()) tma_store_wait_all();
@@ -390,7 +487,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // CTA `rank` of a cluster of `splits` takes k-blocks rank, rank + splits, ... of 128 weight rows (the instruction's rows) and all
 // tokens (its columns, `nt` of them, a multiple of 16).
 constexpr int FEW_ROWS = 128;                     // tokens at most: one scale tile
-constexpr int FEW_THREADS = 64 + 128;
+constexpr int FEW_THREADS = 64 + 32 * 8;              // at most: 8 warps read the accumulators, 4 of up to 32 tokens
 constexpr int FEW_MAX_STAGES = 8;
 struct FewArgs {
   int num_k_blocks, nt, splits;
@@ -401,10 +498,28 @@ struct FewArgs {
   int32_t* status;
   uint64_t wait_limit_ns;
 };
-__device__ __forceinline__ float load_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
+}
+template <int DT>
+__device__ __forceinline__ void put_four_as(const OutArgs& o, int row, int col, const float (&f)[4]) {
+  typedef typename OutOf<DT>::type T;
+  T* p = static_cast<T*>(o.p) + int64_t(row) * o.ld + col;
+  if (o.bulk && !o.accumulate && col + 4 <= o.J) {           // (rows on 16-byte boundaries)
+    if constexpr (DT == FP4_DTYPE_FP32) *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(two_values<DT>(f[0], f[1]), two_values<DT>(f[2], f[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < o.J) p[i] = OutOf<DT>::put(o.accumulate ? f[i] + OutOf<DT>::get(p[i]) : f[i]);
+  }
+}
+__device__ __forceinline__ void put_four(const OutArgs& o, int row, int col, const float (&f)[4]) {
+  if (o.dtype == FP4_DTYPE_BF16) put_four_as<FP4_DTYPE_BF16>(o, row, col, f);
+  else if (o.dtype == FP4_DTYPE_FP16) put_four_as<FP4_DTYPE_FP16>(o, row, col, f);
+  else put_four_as<FP4_DTYPE_FP32>(o, row, col, f);
 }
 template <int FMT>
 __global__ void __launch_bounds__(FEW_THREADS)
@@ -435,6 +550,17 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
+  const auto request = [&](int kb, int stage) {
+    uint8_t* p = smem + stage * STAGE_BYTES;
+    mbar_arrive_expect_tx(&full_bar[stage], args.tx_bytes);
+    tma_load_2d(p, &map_w, &full_bar[stage], kb * 128, j_blk * BM);
+    tma_load_2d(p + A_BYTES + x_bytes, &map_sw, &full_bar[stage], kb * (scale_bytes(FMT) / 8), j_blk);
+    tma_load_2d(p + A_BYTES, &map_x, &full_bar[stage], kb * 128, 0);
+    tma_load_2d(p + A_BYTES + x_bytes + scale_bytes(FMT), &map_sx, &full_bar[stage], kb * (scale_bytes(FMT) / 8), 0);
+  };
+  // The stages are empty and the barriers this thread's own work: the first k-blocks travel while tensor memory is allocated.
+  if (threadIdx.x == 0)
+    for (int s = 0, kb = rank; s < STAGES && kb < args.num_k_blocks; ++s, kb += args.splits) request(kb, s);
   if (warp == 1) tmem_alloc<1>(tmem_slot, args.tmem_cols);
   tc_fence_before();
   __syncthreads();
@@ -447,14 +573,11 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       uint32_t phase = 0, fills = 0;
       bool ok = true;
       for (int kb = rank; kb < args.num_k_blocks; kb += args.splits) {
-        ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
-        if (!ok) break;
-        uint8_t* p = smem + stage * STAGE_BYTES;
-        mbar_arrive_expect_tx(&full_bar[stage], args.tx_bytes);
-        tma_load_2d(p, &map_w, &full_bar[stage], kb * 128, j_blk * BM);
-        tma_load_2d(p + A_BYTES + x_bytes, &map_sw, &full_bar[stage], kb * (scale_bytes(FMT) / 8), j_blk);
-        tma_load_2d(p + A_BYTES, &map_x, &full_bar[stage], kb * 128, 0);
-        tma_load_2d(p + A_BYTES + x_bytes + scale_bytes(FMT), &map_sx, &full_bar[stage], kb * (scale_bytes(FMT) / 8), 0);
+        if (fills >= uint32_t(STAGES)) {
+          ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
+          if (!ok) break;
+          request(kb, stage);
+        }
         ++fills;
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
@@ -497,7 +620,7 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   if (done && warp >= 2) {
     const int quarter = warp & 3;
     const bool any = rank < args.num_k_blocks;             // a CTA without a k-block adds nothing
-    for (int c = 0; c < args.nt; c += 16) {
+    for (int c = 16 * ((warp - 2) >> 2); c < args.nt; c += 4 * (int(blockDim.x) / 32 - 2)) {
       uint32_t v[32];
       tmem_ld_32x16(tmem_base + (uint32_t(quarter * 32) << 16) + uint32_t(c), v);
       tmem_ld_wait();
@@ -510,14 +633,31 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   __syncthreads();
   if (args.splits > 1) cluster_sync_all();
   const float2 scales = tensor_scales(args.powers);
-  for (int e = rank * FEW_THREADS + int(threadIdx.x); e < args.out.I * BM; e += args.splits * FEW_THREADS) {
-    const int token = e / BM, j = j_blk * BM + e % BM;
-    float sum = 0.0f;
-    if (args.splits > 1)
-      for (int s = 0; s < args.splits; ++s) sum += load_cluster(cluster_address(part + e, uint32_t(s)));
-    else
-      sum = part[e];
-    if (j < args.out.J) put_any(args.out.p, int64_t(token) * args.out.ld + j, sum * scales.x * scales.y, args.out.accumulate, args.out.dtype);
+  // four neighbouring columns of a token at a time, and four such fours on their way together
+  constexpr int AT_ONCE = 4;
+  const int step = args.splits * int(blockDim.x), n = args.out.I * (BM / 4);
+  for (int e0 = rank * int(blockDim.x) + int(threadIdx.x); e0 < n; e0 += AT_ONCE * step) {
+    float4 sum[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) sum[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s = 0; s < args.splits; ++s) {
+      const uint32_t from = args.splits > 1 ? cluster_address(part, uint32_t(s)) : smem_u32(part);
+      float4 v[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+        if (e0 + i * step < n) v[i] = load_cluster(from + 16 * uint32_t(e0 + i * step));
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+        if (e0 + i * step < n) { sum[i].x += v[i].x; sum[i].y += v[i].y; sum[i].z += v[i].z; sum[i].w += v[i].w; }
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int e = e0 + i * step;
+      if (e >= n) break;
+      const float f[4] = {sum[i].x * scales.x * scales.y, sum[i].y * scales.x * scales.y, sum[i].z * scales.x * scales.y,
+                          sum[i].w * scales.x * scales.y};
+      put_four(args.out, e / (BM / 4), j_blk * BM + e % (BM / 4) * 4, f);
+    }
   }
   if (args.splits > 1) cluster_sync_all();                 // nobody leaves while others read its part
   if (warp == 1) tmem_dealloc<1>(tmem_base, args.tmem_cols);
@@ -552,7 +692,7 @@ OutArgs out_args(const MxGemm& g) {
   const int64_t elt = g.dtype == FP4_DTYPE_FP32 ? 4 : 2;
   OutArgs o = {g.out, g.ld, int(g.I), int(g.J), g.dtype, g.accumulate, false};
   // (a bulk store clips a row at its map's end to whole 16 bytes: a row that ends inside such a piece would take its neighbours' bytes along)
-  o.bulk = !g.accumulate && (reinterpret_cast<uintptr_t>(g.out) & 15) == 0 && (g.ld * elt) % 16 == 0 && (g.J * elt) % 16 == 0;
+  o.bulk = (reinterpret_cast<uintptr_t>(g.out) & 15) == 0 && (g.ld * elt) % 16 == 0 && (g.J * elt) % 16 == 0;
   return o;
 }
 Powers powers_of(const MxGemm& g) {
@@ -561,32 +701,53 @@ Powers powers_of(const MxGemm& g) {
 }
 uint64_t wait_limit(const fp4_ctx* ctx) { return ctx->debug_wait_limit_ns ? ctx->debug_wait_limit_ns : WAIT_LIMIT_NS; }
 
+// Times (ns) of the forms, as a model: a launch, then for each tile of the busiest worker a fixed part and one per k-block.  Fitted to
+// 21 sizes from 256 x 256 x 8192 to 4096 x 4096 x 4096 in all forms (within 5 % by root mean square, 16 % at worst; blocks of 16 cost a tenth
+// more per k-block).  One thread issues a k-block's copies of scales and MMAs in 250 ns, whatever the width, so narrow tiles pay only where
+// they fill SMs that would idle: 1024^3 4.8 us by 128 x 64 against 6.4 by pairs 256 wide, 4096 x 2048 x 5504 45 against 19.5.
 struct TileForm {
   int bn;
   bool pair;
+  int64_t cost;
 };
-// The form whose busiest worker ends first: tiles of a worker x (what a tile costs beside its k-blocks + k-blocks x time of one).
+struct FormCost {
+  int bn;
+  bool pair;
+  int launch, tile, k_block;
+};
+constexpr FormCost FORMS[] = {{64, false, 3400, 460, 251},  {128, false, 3400, 650, 270},  {192, false, 3400, 1030, 296}, {256, false, 3400, 1640, 344},
+                              {128, true, 4000, 700, 228}, {192, true, 4000, 1030, 239}, {256, true, 4000, 1460, 279}};
 TileForm choose_form(const fp4_ctx* ctx, const MxGemm& g) {
   const int64_t kbs = (g.C + 255) / 256;
-  TileForm best = {64, false};
-  int64_t best_cost = -1;
-  for (const bool pair : {false, true})
-    for (const int bn : {64, 128, 192}) {
-      if (pair && (bn == 64 || ctx->num_sms < 2)) continue;
-      const int64_t rows = pair ? 2 * BM : BM, workers = pair ? ctx->num_sms / 2 : ctx->num_sms;
-      const int64_t tiles = (g.I + rows - 1) / rows * ((g.J + bn - 1) / bn), rounds = (tiles + workers - 1) / workers;
-      const int64_t mma = pair ? 1300 + kbs * (105 + (83 * bn) / 100) : 800 + kbs * (170 + (17 * bn) / 20), epi = 10 * bn + (pair ? 900 : 0);
-      const int64_t cost = rounds * (mma > epi ? mma : epi) + (mma > epi ? epi : mma) + (pair ? 1000 : 0);
-      if (best_cost < 0 || cost < best_cost) {
-        best_cost = cost;
-        best = {bn, pair};
-      }
-    }
+  TileForm best = {64, false, -1};
+  for (const FormCost& f : FORMS) {
+    const int64_t rows = f.pair ? 2 * BM : BM, workers = f.pair ? ctx->num_sms / 2 : ctx->num_sms;
+    if (!workers) continue;
+    const int64_t rounds = ((g.I + rows - 1) / rows * ((g.J + f.bn - 1) / f.bn) + workers - 1) / workers;
+    const int64_t cost = f.launch + rounds * (f.tile + kbs * f.k_block * (g.format == FP4_MX_NVFP4 ? 11 : 10) / 10);
+    if (best.cost < 0 || cost < best.cost) best = {f.bn, f.pair, cost};
+  }
   return best;
 }
 
-template <int FMT, bool PAIR>
-int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int32_t* status) {
+// Few rows: into how many parts a cluster splits the contraction, and the time by the same kind of model.  More than four parts, or more CTAs
+// than SMs, cost more than they save (clusters of 8 do not fill the GPU: 1 x 4096 x 4096 5.0 us in 4 parts, 7.3 in 8; not split 6.8).
+struct FewForm {
+  int splits;
+  int64_t cost;
+};
+FewForm choose_few(const fp4_ctx* ctx, const MxGemm& g) {
+  const int64_t kbs = (g.C + 255) / 256, tiles = (g.J + BM - 1) / BM;
+  int64_t splits = ctx->num_sms / tiles;
+  if (splits > (kbs + 1) / 2) splits = (kbs + 1) / 2;
+  splits = splits < 1 ? 1 : (splits > 4 ? 4 : splits);
+  const int64_t rounds = (tiles + 2 * ctx->num_sms - 1) / (2 * ctx->num_sms);
+  const int64_t one = (kbs + splits - 1) / splits * (g.format == FP4_MX_NVFP4 ? 200 : 150) + 15 * ((g.I + 15) / 16 * 16);
+  return {int(splits), 4100 + (splits > 1 ? 300 : 0) + rounds * one};
+}
+
+template <int FMT, bool PAIR, int DT>
+int launch_tiles_as(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int32_t* status) {
   constexpr int CTAS = PAIR ? 2 : 1;
   CUtensorMap a, b, sa, sb, out = {};
   GemmArgs args = {};
@@ -617,8 +778,8 @@ int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int
                   CU_TENSOR_MAP_L2_PROMOTION_NONE);
   }
   if (rc != FP4_OK) return rc;
-  const auto kernel = mx_gemm_kernel<FMT, PAIR>;
-  FP4_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST_SMEM));
+  constexpr auto kernel = mx_gemm_kernel<FMT, PAIR, DT>;
+  FP4_CUDA_TRY(mx_allow_smem<kernel>(ctx->device, MOST_SMEM));
   const int64_t tiles = int64_t(args.num_m_blocks) * args.num_n_blocks, most = ctx->num_sms / CTAS;
   cudaLaunchAttribute cluster = {};
   cluster.id = cudaLaunchAttributeClusterDimension;
@@ -636,19 +797,24 @@ int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int
   return FP4_OK;
 }
 
+template <int FMT, bool PAIR>
+int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int32_t* status) {
+  if (g.dtype == FP4_DTYPE_BF16) return launch_tiles_as<FMT, PAIR, FP4_DTYPE_BF16>(ctx, stream, g, bn, status);
+  if (g.dtype == FP4_DTYPE_FP16) return launch_tiles_as<FMT, PAIR, FP4_DTYPE_FP16>(ctx, stream, g, bn, status);
+  return launch_tiles_as<FMT, PAIR, FP4_DTYPE_FP32>(ctx, stream, g, bn, status);
+}
+
 template <int FMT>
-int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* status) {
+int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, int32_t* status) {
   CUtensorMap w, x, sw, sx;
   FewArgs args = {};
   args.num_k_blocks = int((g.C + 255) / 256);
   args.nt = int((g.I + 15) / 16 * 16);
   const int tiles = int((g.J + BM - 1) / BM);
-  // as many parts of the contraction as fill the SMs once, at most a portable cluster
-  args.splits = ctx->num_sms / tiles;
-  if (args.splits > args.num_k_blocks) args.splits = args.num_k_blocks;
-  args.splits = args.splits < 1 ? 1 : (args.splits > 8 ? 8 : args.splits);
+  args.splits = splits;
   args.stage_bytes = A_BYTES + args.nt * 128 + 2 * scale_bytes(FMT);
-  args.stages = (MOST_SMEM - 1024 - MISC_BYTES) / args.stage_bytes;
+  // (more CTAs than SMs: two on each)
+  args.stages = ((tiles > ctx->num_sms ? 113 * 1024 : MOST_SMEM) - 1024 - MISC_BYTES) / args.stage_bytes;
   if (args.stages > FEW_MAX_STAGES) args.stages = FEW_MAX_STAGES;
   const int per_cta = (args.num_k_blocks + args.splits - 1) / args.splits;
   if (args.stages > per_cta) args.stages = per_cta;
@@ -666,15 +832,15 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* stat
   if (rc == FP4_OK) rc = make_scales_map(ctx, &sw, g.b_scales, g.J, g.C, FMT, 1);
   if (rc == FP4_OK) rc = make_scales_map(ctx, &sx, g.a_scales, g.I, g.C, FMT, 1);
   if (rc != FP4_OK) return rc;
-  const auto kernel = mx_gemm_few_kernel<FMT>;
-  FP4_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST_SMEM));
+  constexpr auto kernel = mx_gemm_few_kernel<FMT>;
+  FP4_CUDA_TRY(mx_allow_smem<kernel>(ctx->device, MOST_SMEM));
   cudaLaunchAttribute cluster = {};
   cluster.id = cudaLaunchAttributeClusterDimension;
   cluster.val.clusterDim.x = unsigned(args.splits);
   cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(tiles * args.splits));
-  cfg.blockDim = dim3(FEW_THREADS);
+  cfg.blockDim = dim3(unsigned(args.nt <= 32 ? FEW_THREADS - 128 : FEW_THREADS));
   cfg.dynamicSmemBytes = size_t(1024 + MISC_BYTES + args.stages * args.stage_bytes);
   cfg.stream = stream;
   cfg.attrs = &cluster;
@@ -688,8 +854,11 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* stat
 
 int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* status) {
   const bool nv = g.format == FP4_MX_NVFP4;
-  if (g.I <= FEW_ROWS) return nv ? launch_few<FP4_MX_NVFP4>(ctx, stream, g, status) : launch_few<FP4_MX_E2M1>(ctx, stream, g, status);
   const TileForm f = choose_form(ctx, g);
+  if (g.I <= FEW_ROWS) {
+    const FewForm few = choose_few(ctx, g);
+    if (few.cost <= f.cost) return nv ? launch_few<FP4_MX_NVFP4>(ctx, stream, g, few.splits, status) : launch_few<FP4_MX_E2M1>(ctx, stream, g, few.splits, status);
+  }
   if (f.pair) return nv ? launch_tiles<FP4_MX_NVFP4, true>(ctx, stream, g, f.bn, status) : launch_tiles<FP4_MX_E2M1, true>(ctx, stream, g, f.bn, status);
   return nv ? launch_tiles<FP4_MX_NVFP4, false>(ctx, stream, g, f.bn, status) : launch_tiles<FP4_MX_E2M1, false>(ctx, stream, g, f.bn, status);
 }

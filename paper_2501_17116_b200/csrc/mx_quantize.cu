@@ -645,23 +645,23 @@ Codes codes_across(const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
   (void)cols;
   return {q.codes_t, q.scales_t, mx_pitch(rows, q.format), mx_tiles(rows)};
 }
-template <class K, class A>
-int launch_tiles(K kernel, int64_t rows, int64_t cols, size_t smem, cudaStream_t stream, const A& args) {
+template <auto KERNEL, class A>
+int launch_tiles(int device, int64_t rows, int64_t cols, size_t smem, cudaStream_t stream, const A& args) {
   const int64_t n = mx_tiles(rows) * mx_tiles(cols);
   if (n > 0x7FFFFFFF) return FP4_ERR_SHAPE;
   if (smem > 40 * 1024)
-    FP4_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
-  kernel<<<unsigned(n), THREADS, smem, stream>>>(args);
+    FP4_CUDA_TRY(mx_allow_smem<KERNEL>(device, int(smem)));
+  KERNEL<<<unsigned(n), THREADS, smem, stream>>>(args);
   FP4_CUDA_TRY(cudaGetLastError());
   return FP4_OK;
 }
 
 template <class T, int FMT>
-int quantize_as(cudaStream_t stream, const QuantArgs& a) {
+int quantize_as(int device, cudaStream_t stream, const QuantArgs& a) {
   const size_t smem = MX_TILE * MX_TILE * sizeof(T);
-  if (a.along.codes && a.across.codes) return launch_tiles(mx_quantize_kernel<T, FMT, true, true>, a.rows, a.cols, smem, stream, a);
-  if (a.across.codes) return launch_tiles(mx_quantize_kernel<T, FMT, false, true>, a.rows, a.cols, smem, stream, a);
-  return launch_tiles(mx_quantize_kernel<T, FMT, true, false>, a.rows, a.cols, 0, stream, a);
+  if (a.along.codes && a.across.codes) return launch_tiles<mx_quantize_kernel<T, FMT, true, true>>(device, a.rows, a.cols, smem, stream, a);
+  if (a.across.codes) return launch_tiles<mx_quantize_kernel<T, FMT, false, true>>(device, a.rows, a.cols, smem, stream, a);
+  return launch_tiles<mx_quantize_kernel<T, FMT, true, false>>(device, a.rows, a.cols, 0, stream, a);
 }
 template <class T>
 int quantize_from(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a, const fp4_mx_tensor& q) {
@@ -673,35 +673,35 @@ int quantize_from(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a, const f
     FP4_CUDA_TRY(cudaGetLastError());
   }
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (q.format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(stream, a);
-  if (q.format == FP4_MX_NVFP4) return quantize_as<T, FP4_MX_NVFP4>(stream, a);
-  return quantize_as<T, FP4_MX_E4M3>(stream, a);
+  if (q.format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(ctx->device, stream, a);
+  if (q.format == FP4_MX_NVFP4) return quantize_as<T, FP4_MX_NVFP4>(ctx->device, stream, a);
+  return quantize_as<T, FP4_MX_E4M3>(ctx->device, stream, a);
 }
 
 template <class T>
-int dequantize_to(cudaStream_t stream, const DequantArgs& a, int format) {
-  if (format == FP4_MX_E2M1) return launch_tiles(mx_dequantize_kernel<T, FP4_MX_E2M1>, a.rows, a.cols, 0, stream, a);
-  if (format == FP4_MX_NVFP4) return launch_tiles(mx_dequantize_kernel<T, FP4_MX_NVFP4>, a.rows, a.cols, 0, stream, a);
-  return launch_tiles(mx_dequantize_kernel<T, FP4_MX_E4M3>, a.rows, a.cols, 0, stream, a);
+int dequantize_to(int device, cudaStream_t stream, const DequantArgs& a, int format) {
+  if (format == FP4_MX_E2M1) return launch_tiles<mx_dequantize_kernel<T, FP4_MX_E2M1>>(device, a.rows, a.cols, 0, stream, a);
+  if (format == FP4_MX_NVFP4) return launch_tiles<mx_dequantize_kernel<T, FP4_MX_NVFP4>>(device, a.rows, a.cols, 0, stream, a);
+  return launch_tiles<mx_dequantize_kernel<T, FP4_MX_E4M3>>(device, a.rows, a.cols, 0, stream, a);
 }
 
 template <class T>
-int swiglu_as(cudaStream_t stream, const SwigluArgs& a, bool bwd, bool keep) {
+int swiglu_as(int device, cudaStream_t stream, const SwigluArgs& a, bool bwd, bool keep) {
   const size_t smem = a.across.codes ? MX_TILE * MX_TILE * sizeof(T) : 0;
   if (bwd)
-    return smem ? launch_tiles(mx_swiglu_kernel<T, true, false, true>, a.rows, a.cols, smem, stream, a)
-                : launch_tiles(mx_swiglu_kernel<T, true, false, false>, a.rows, a.cols, 0, stream, a);
+    return smem ? launch_tiles<mx_swiglu_kernel<T, true, false, true>>(device, a.rows, a.cols, smem, stream, a)
+                : launch_tiles<mx_swiglu_kernel<T, true, false, false>>(device, a.rows, a.cols, 0, stream, a);
   if (keep)
-    return smem ? launch_tiles(mx_swiglu_kernel<T, false, true, true>, a.rows, a.cols, smem, stream, a)
-                : launch_tiles(mx_swiglu_kernel<T, false, true, false>, a.rows, a.cols, 0, stream, a);
-  return smem ? launch_tiles(mx_swiglu_kernel<T, false, false, true>, a.rows, a.cols, smem, stream, a)
-              : launch_tiles(mx_swiglu_kernel<T, false, false, false>, a.rows, a.cols, 0, stream, a);
+    return smem ? launch_tiles<mx_swiglu_kernel<T, false, true, true>>(device, a.rows, a.cols, smem, stream, a)
+                : launch_tiles<mx_swiglu_kernel<T, false, true, false>>(device, a.rows, a.cols, 0, stream, a);
+  return smem ? launch_tiles<mx_swiglu_kernel<T, false, false, true>>(device, a.rows, a.cols, smem, stream, a)
+              : launch_tiles<mx_swiglu_kernel<T, false, false, false>>(device, a.rows, a.cols, 0, stream, a);
 }
 int swiglu(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, int dtype, bool bwd, bool keep) {
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (dtype == FP4_DTYPE_BF16) return swiglu_as<__nv_bfloat16>(stream, a, bwd, keep);
-  if (dtype == FP4_DTYPE_FP16) return swiglu_as<__half>(stream, a, bwd, keep);
-  return swiglu_as<float>(stream, a, bwd, keep);
+  if (dtype == FP4_DTYPE_BF16) return swiglu_as<__nv_bfloat16>(ctx->device, stream, a, bwd, keep);
+  if (dtype == FP4_DTYPE_FP16) return swiglu_as<__half>(ctx->device, stream, a, bwd, keep);
+  return swiglu_as<float>(ctx->device, stream, a, bwd, keep);
 }
 
 }  // namespace
@@ -726,9 +726,9 @@ int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes
                          int64_t rows, int64_t cols, int format, void* out, int64_t ld, int dtype) {
   const DequantArgs a = {codes, scales, reinterpret_cast<const uint32_t*>(amax), rows, cols, out, ld, rows_aligned(out, ld, dtype)};
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (dtype == FP4_DTYPE_BF16) return dequantize_to<__nv_bfloat16>(stream, a, format);
-  if (dtype == FP4_DTYPE_FP16) return dequantize_to<__half>(stream, a, format);
-  return dequantize_to<float>(stream, a, format);
+  if (dtype == FP4_DTYPE_BF16) return dequantize_to<__nv_bfloat16>(ctx->device, stream, a, format);
+  if (dtype == FP4_DTYPE_FP16) return dequantize_to<__half>(ctx->device, stream, a, format);
+  return dequantize_to<float>(ctx->device, stream, a, format);
 }
 
 int launch_mx_swiglu_fwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix gate, MxMatrix up, int64_t rows, int64_t cols, int dtype,

@@ -55,17 +55,18 @@ def declare(lib: C.CDLL):
         f.argtypes, f.restype = [vp, vp] + args, i32
 
 
-def _stream(ctx: Context):
-    return torch._C._cuda_getCurrentRawStream(ctx.device)
+_stream_of = torch._C._cuda_getCurrentRawStream
+_byref = C.byref
 
 
 def _matrix(ctx: Context, t):
     """Structure of a matrix (None: of none)."""
     if t is None:
         return None
-    assert t.dim() == 2 and t.is_cuda and t.device.index == ctx.device and t.dtype in _DTYPES
-    assert t.shape[1] <= 1 or t.stride(1) == 1
-    return C.byref(fp4_mx_matrix(t.data_ptr(), t.stride(0), _DTYPES[t.dtype], 0))
+    stride, dtype = t.stride(), _DTYPES.get(t.dtype)
+    assert dtype is not None and len(stride) == 2 and t.get_device() == ctx.device
+    assert stride[1] == 1 or t.shape[1] <= 1
+    return _byref(fp4_mx_matrix(t.data_ptr(), stride[0], dtype, 0))
 
 
 def _new(ctx: Context, rows: int, cols: int, dtype):
@@ -88,6 +89,7 @@ class MXTensor:
         where = lambda t: None if t is None else (t.data_ptr() or 16)                         # noqa: E731
         self.struct = fp4_mx_tensor(rows, cols, where(self.codes), where(self.scales), where(self.codes_t), where(self.scales_t),
                                     _ptr(self.amax), fmt, 0)
+        self.ref = _byref(self.struct)
 
 
 class SwigluCheckpoint:
@@ -98,26 +100,21 @@ class SwigluCheckpoint:
         self.up = MXTensor(rows, cols, device, fmt=FP4_MX_E4M3)
 
 
-def _tensor(q):
-    return None if q is None else C.byref(q.struct)
-
-
 def fp4_mx_quantize(ctx: Context, x: torch.Tensor, fmt: int = FP4_MX_E2M1, codes: bool = True, codes_t: bool = False,
                     out: MXTensor | None = None, amax: torch.Tensor | None = None) -> MXTensor:
     """`x` in blocks along its columns (`codes`) and / or its rows (`codes_t`).  `amax` (FP4_MX_NVFP4; one float on the
     device) is taken for the tensor's largest magnitude instead of looking for it."""
-    rows, cols = x.shape
     if out is None:
-        out = MXTensor(rows, cols, x.device, fmt, codes, codes_t)
-    assert (out.rows, out.cols) == (rows, cols)
-    out.struct.flags = 0
-    if amax is not None and out.amax is not None:
+        out = MXTensor(*x.shape, x.device, fmt, codes, codes_t)
+    assert x.shape == (out.rows, out.cols)
+    given = amax is not None and out.amax is not None
+    if given:
         out.amax.copy_(amax.reshape(1))
         out.struct.flags = FP4_MX_AMAX_GIVEN
-    try:
-        _check(ctx.lib.fp4_mx_quantize(ctx.handle, _stream(ctx), _matrix(ctx, x), _tensor(out), _ptr(ctx.status)))
-    finally:
+    rc = ctx.lib.fp4_mx_quantize(ctx.handle, _stream_of(ctx.device), _matrix(ctx, x), out.ref, ctx.status.data_ptr())
+    if given:
         out.struct.flags = 0
+    _check(rc)
     return out
 
 
@@ -127,8 +124,8 @@ def fp4_mx_dequantize(ctx: Context, q: MXTensor, transposed: bool = False, dtype
     shape = (q.cols, q.rows) if transposed else (q.rows, q.cols)
     if out is None:
         out = _new(ctx, *shape, dtype)
-    assert tuple(out.shape) == shape
-    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream(ctx), _tensor(q), int(transposed), _matrix(ctx, out)))
+    assert out.shape == shape
+    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream_of(ctx.device), q.ref, int(transposed), _matrix(ctx, out)))
     return out
 
 
@@ -139,9 +136,9 @@ def fp4_mx_gemm(ctx: Context, a: MXTensor, b: MXTensor, a_t: bool = False, b_t: 
     if out is None:
         assert not accumulate
         out = _new(ctx, *shape, dtype)
-    assert tuple(out.shape) == shape
+    assert out.shape == shape
     flags = (FP4_MX_A_T if a_t else 0) | (FP4_MX_B_T if b_t else 0) | (FP4_MX_ACCUMULATE if accumulate else 0)
-    _check(ctx.lib.fp4_mx_gemm(ctx.handle, _stream(ctx), _tensor(a), _tensor(b), flags, _matrix(ctx, out), _ptr(ctx.status)))
+    _check(ctx.lib.fp4_mx_gemm(ctx.handle, _stream_of(ctx.device), a.ref, b.ref, flags, _matrix(ctx, out), ctx.status.data_ptr()))
     return out
 
 
@@ -163,11 +160,11 @@ def fp4_mx_linear_fwd(ctx: Context, X: torch.Tensor | None, W: torch.Tensor | No
         assert (saved_w.rows, saved_w.cols) == (K, N)
     if out is None:
         out = _new(ctx, M, N, dtype or (X.dtype if X is not None else torch.bfloat16))
-    assert tuple(out.shape) == (M, N)
+    assert out.shape == (M, N)
     reuse = (FP4_REUSE_X if reuse_x else 0) | (FP4_REUSE_W if reuse_w else 0)
-    _check(ctx.lib.fp4_mx_linear_fwd(ctx.handle, _stream(ctx), None if reuse_x else _matrix(ctx, X),
+    _check(ctx.lib.fp4_mx_linear_fwd(ctx.handle, _stream_of(ctx.device), None if reuse_x else _matrix(ctx, X),
                                      None if reuse_w else _matrix(ctx, W), M, K, N, reuse, _matrix(ctx, out),
-                                     _tensor(saved_x), _tensor(saved_w), _ptr(ctx.status)))
+                                     saved_x.ref, saved_w.ref, ctx.status.data_ptr()))
     return out, saved_x, saved_w
 
 
@@ -183,37 +180,43 @@ def fp4_mx_linear_bwd(ctx: Context, dY: torch.Tensor, saved_x: MXTensor, saved_w
     if dW is None and want_dw:
         assert not accumulate_dw
         dW = _new(ctx, K, N, dtype or dY.dtype)
-    assert (dX is None or tuple(dX.shape) == (M, K)) and (dW is None or tuple(dW.shape) == (K, N))
+    assert (dX is None or dX.shape == (M, K)) and (dW is None or dW.shape == (K, N))
     flags = (FP4_MX_ACCUMULATE_DX if accumulate_dx else 0) | (FP4_MX_ACCUMULATE_DW if accumulate_dw else 0)
-    _check(ctx.lib.fp4_mx_linear_bwd(ctx.handle, _stream(ctx), _matrix(ctx, dY), _tensor(saved_x), _tensor(saved_w), M, K, N,
-                                     flags, _matrix(ctx, dX), _matrix(ctx, dW), _ptr(ctx.status)))
+    _check(ctx.lib.fp4_mx_linear_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dY), saved_x.ref, saved_w.ref, M, K, N,
+                                     flags, _matrix(ctx, dX), _matrix(ctx, dW), ctx.status.data_ptr()))
     return dX, dW
 
 
 def fp4_mx_swiglu_fwd(ctx: Context, gate: torch.Tensor, up: torch.Tensor, out: torch.Tensor | None = None,
                       checkpoint: SwigluCheckpoint | None = None, quantized: MXTensor | None = None, want_h: bool = True):
     """h = gate * sigmoid(gate) * up, the inputs in 8 bits into `checkpoint`, h as an operand into `quantized`."""
-    rows, cols = gate.shape
-    assert tuple(up.shape) == (rows, cols)
+    shape = rows, cols = gate.shape
     if out is None and want_h:
         out = _new(ctx, rows, cols, gate.dtype)
-    assert out is None or tuple(out.shape) == (rows, cols)
-    c = checkpoint
-    assert all(q is None or (q.rows, q.cols) == (rows, cols) for q in (c and c.gate, c and c.up, quantized))
-    _check(ctx.lib.fp4_mx_swiglu_fwd(ctx.handle, _stream(ctx), _matrix(ctx, gate), _matrix(ctx, up), rows, cols, _matrix(ctx, out),
-                                     _tensor(c and c.gate), _tensor(c and c.up), _tensor(quantized), _ptr(ctx.status)))
+    assert up.shape == shape and (out is None or out.shape == shape)
+    g = u = q = None
+    if checkpoint is not None:
+        assert (checkpoint.gate.rows, checkpoint.gate.cols) == shape
+        g, u = checkpoint.gate.ref, checkpoint.up.ref
+    if quantized is not None:
+        assert (quantized.rows, quantized.cols) == shape
+        q = quantized.ref
+    _check(ctx.lib.fp4_mx_swiglu_fwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, gate), _matrix(ctx, up), rows, cols,
+                                     _matrix(ctx, out), g, u, q, ctx.status.data_ptr()))
     return out, checkpoint, quantized
 
 
 def fp4_mx_swiglu_bwd(ctx: Context, dh: torch.Tensor, checkpoint: SwigluCheckpoint, dgate: torch.Tensor | None = None,
                       dup: torch.Tensor | None = None, h: torch.Tensor | None = None, quantized: MXTensor | None = None):
     """d_gate and d_up from the checkpoint; h made again into `h` and / or, as an operand, into `quantized`."""
-    rows, cols = dh.shape
+    shape = rows, cols = dh.shape
     dgate = _new(ctx, rows, cols, dh.dtype) if dgate is None else dgate
     dup = _new(ctx, rows, cols, dh.dtype) if dup is None else dup
-    assert all(t is None or tuple(t.shape) == (rows, cols) for t in (dgate, dup, h))
-    assert quantized is None or (quantized.rows, quantized.cols) == (rows, cols)
-    _check(ctx.lib.fp4_mx_swiglu_bwd(ctx.handle, _stream(ctx), _matrix(ctx, dh), _tensor(checkpoint.gate), _tensor(checkpoint.up),
-                                     rows, cols, _matrix(ctx, dgate), _matrix(ctx, dup), _matrix(ctx, h), _tensor(quantized),
-                                     _ptr(ctx.status)))
+    assert dgate.shape == shape and dup.shape == shape and (h is None or h.shape == shape)
+    q = None
+    if quantized is not None:
+        assert (quantized.rows, quantized.cols) == shape
+        q = quantized.ref
+    _check(ctx.lib.fp4_mx_swiglu_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dh), checkpoint.gate.ref, checkpoint.up.ref, rows, cols,
+                                     _matrix(ctx, dgate), _matrix(ctx, dup), _matrix(ctx, h), q, ctx.status.data_ptr()))
     return dgate, dup
