@@ -430,7 +430,7 @@ int fp4_mx_quantize(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, fp4_mx_t
 /* The values that the codes stand for, rounded once to out's type: [rows x cols] from `codes`, or with
  * transposed != 0 [cols x rows] from `codes_t`.  (A value within its last rounding step of the type's
  * largest may come out as infinity.)                                                                    */
-int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int transposed, const fp4_mx_matrix* out);
+int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int transposed, const fp4_mx_matrix* out, int32_t* status);
 
 /* out[i, j] = g_a g_b sum_c a[i, c] b[j, c], fp32 sums, rounded once; with FP4_MX_ACCUMULATE the former value
  * of out is added before the rounding.  `a` is [I x C]: the tensor's rows (`codes`), or with FP4_MX_A_T its

@@ -49,6 +49,32 @@ cudaError_t mx_allow_smem(int device, int bytes) {
   return e;
 }
 
+// The kernels are launched so that one may start while the one before it on the stream drains (programmatic dependent launch): it sets
+// itself up and waits here, ahead of its first access to global memory, until everything before it is complete and visible.
+__device__ __forceinline__ void mx_wait_for_inputs() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Behind that, when the block holds all that it needs of its SM (tensor memory!): the next kernel's blocks may come, and must not get hold of
+// what a block that they wait for is still to be given.
+__device__ __forceinline__ void mx_let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// `cluster` CTAs a cluster.
+template <auto KERNEL, class... A>
+int mx_launch(dim3 grid, int threads, int smem, int cluster, cudaStream_t stream, const A&... args) {
+  cudaLaunchAttribute attrs[2] = {};
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = unsigned(cluster);
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = size_t(smem);
+  cfg.stream = stream;
+  cfg.attrs = attrs;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  FP4_CUDA_TRY(cudaLaunchKernelEx(&cfg, KERNEL, args...));
+  return FP4_OK;
+}
+
 struct MxMatrix {               // a matrix of the caller's: rows of `ld` elements
   const void* p;
   int64_t ld;
@@ -56,7 +82,7 @@ struct MxMatrix {               // a matrix of the caller's: rows of `ld` elemen
 
 int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, MxMatrix x, int dtype, const fp4_mx_tensor& q, int32_t* status);
 int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes, const uint8_t* scales, const float* amax,
-                         int64_t rows, int64_t cols, int format, void* out, int64_t ld, int dtype);
+                         int64_t rows, int64_t cols, int format, MxMatrix out, int dtype, int32_t* status);
 // `h` may have no pointer; `q` (may be null): E2M1 in blocks of 32.
 int launch_mx_swiglu_fwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix gate, MxMatrix up, int64_t rows, int64_t cols, int dtype,
                          MxMatrix h, const fp4_mx_tensor* ckpt_gate, const fp4_mx_tensor* ckpt_up, const fp4_mx_tensor* q,

@@ -120,8 +120,8 @@ int fp4_mx_quantize(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, fp4_mx_t
   return quantize(ctx, static_cast<cudaStream_t>(stream), x, *out, status);
 }
 
-int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int transposed, const fp4_mx_matrix* out) {
-  if (!ctx || !q || !out) return FP4_ERR_NULL;
+int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int transposed, const fp4_mx_matrix* out, int32_t* status) {
+  if (!ctx || !q || !out || !status) return FP4_ERR_NULL;
   std::lock_guard<std::mutex> turn(ctx->mutex);
   const int64_t rows = transposed ? q->cols : q->rows, cols = transposed ? q->rows : q->cols;
   int rc = check_sizes(rows, cols);
@@ -133,7 +133,7 @@ int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int tr
   if (!device.ok) return FP4_ERR_CUDA;
   const MxMatrix o = matrix(out, rows, cols);
   return launch_mx_dequantize(ctx, static_cast<cudaStream_t>(stream), transposed ? q->codes_t : q->codes,
-                              transposed ? q->scales_t : q->scales, q->amax, rows, cols, q->format, out->data, o.ld, out->dtype);
+                              transposed ? q->scales_t : q->scales, q->amax, rows, cols, q->format, o, out->dtype, status);
 }
 
 int fp4_mx_gemm(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* a, const fp4_mx_tensor* b, int flags,

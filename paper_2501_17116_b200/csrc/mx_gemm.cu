@@ -360,13 +360,15 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes, &map_sa, bar, kb * (scale_bytes(FMT) / 8), m_blk);
     tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes + scale_bytes(FMT), &map_sb, bar, kb * (scale_bytes(FMT) / 8), n0 / 128);
   };
-  // Single CTAs: the stages are empty and the barriers this thread's own work, so the first tile's first k-blocks travel while tensor
-  // memory is allocated.  (A pair's barriers have to be known to exist first.)
+  if (warp == 1) tmem_alloc<CTAS>(tmem_slot, TMEM_COLS);
+  mx_wait_for_inputs();
+  // Single CTAs: the stages are empty and the barriers this thread's own work, so the first tile's first k-blocks travel while the
+  // others meet.  (A pair's barriers have to be known to exist first.)
   if (!PAIR && threadIdx.x == 0 && worker < num_tiles)
     for (int s = 0; s < STAGES && s < args.num_k_blocks; ++s) request(worker % args.num_m_blocks, worker / args.num_m_blocks * args.bn, s, s);
-  if (warp == 1) tmem_alloc<CTAS>(tmem_slot, TMEM_COLS);
   tc_fence_before();
   __syncthreads();
+  mx_let_next_start();
   if (PAIR) cluster_sync_all();               // the peer's barriers exist
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
@@ -489,6 +491,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 constexpr int FEW_ROWS = 128;                     // tokens at most: one scale tile
 constexpr int FEW_THREADS = 64 + 32 * 8;              // at most: 8 warps read the accumulators, 4 of up to 32 tokens
 constexpr int FEW_MAX_STAGES = 8;
+constexpr int FEW_LEAST_SMEM = 78 * 1024;
 struct FewArgs {
   int num_k_blocks, nt, splits;
   int stages, stage_bytes;
@@ -558,12 +561,14 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     tma_load_2d(p + A_BYTES, &map_x, &full_bar[stage], kb * 128, 0);
     tma_load_2d(p + A_BYTES + x_bytes + scale_bytes(FMT), &map_sx, &full_bar[stage], kb * (scale_bytes(FMT) / 8), 0);
   };
-  // The stages are empty and the barriers this thread's own work: the first k-blocks travel while tensor memory is allocated.
+  if (warp == 1) tmem_alloc<1>(tmem_slot, args.tmem_cols);
+  mx_wait_for_inputs();
+  // The stages are empty and the barriers this thread's own work: the first k-blocks travel while the others meet.
   if (threadIdx.x == 0)
     for (int s = 0, kb = rank; s < STAGES && kb < args.num_k_blocks; ++s, kb += args.splits) request(kb, s);
-  if (warp == 1) tmem_alloc<1>(tmem_slot, args.tmem_cols);
   tc_fence_before();
   __syncthreads();
+  mx_let_next_start();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
@@ -781,20 +786,9 @@ int launch_tiles_as(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, 
   constexpr auto kernel = mx_gemm_kernel<FMT, PAIR, DT>;
   FP4_CUDA_TRY(mx_allow_smem<kernel>(ctx->device, MOST_SMEM));
   const int64_t tiles = int64_t(args.num_m_blocks) * args.num_n_blocks, most = ctx->num_sms / CTAS;
-  cudaLaunchAttribute cluster = {};
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = 2;
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(CTAS * (tiles < most ? tiles : most)));
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = size_t(FIXED_SMEM + args.stages * args.stage_bytes);
-  cfg.stream = stream;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = PAIR ? 1 : 0;
   KernelScope scope(ctx, stream, KC_GEMM, 1);
-  FP4_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, b, sa, sb, out, args));
-  return FP4_OK;
+  return mx_launch<kernel>(dim3(unsigned(CTAS * (tiles < most ? tiles : most))), THREADS, FIXED_SMEM + args.stages * args.stage_bytes, CTAS, stream, a, b,
+                           sa, sb, out, args);
 }
 
 template <int FMT, bool PAIR>
@@ -834,20 +828,12 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, i
   if (rc != FP4_OK) return rc;
   constexpr auto kernel = mx_gemm_few_kernel<FMT>;
   FP4_CUDA_TRY(mx_allow_smem<kernel>(ctx->device, MOST_SMEM));
-  cudaLaunchAttribute cluster = {};
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = unsigned(args.splits);
-  cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(tiles * args.splits));
-  cfg.blockDim = dim3(unsigned(args.nt <= 32 ? FEW_THREADS - 128 : FEW_THREADS));
-  cfg.dynamicSmemBytes = size_t(1024 + MISC_BYTES + args.stages * args.stage_bytes);
-  cfg.stream = stream;
-  cfg.attrs = &cluster;
-  cfg.numAttrs = args.splits > 1 ? 1 : 0;
+  // At least a third of an SM's shared memory: two CTAs an SM find their 256 columns of tensor memory, a third one would wait for
+  // theirs, and CTAs of clusters that wait so for one another would wait for good.
+  int smem = 1024 + MISC_BYTES + args.stages * args.stage_bytes;
+  if (smem < FEW_LEAST_SMEM) smem = FEW_LEAST_SMEM;
   KernelScope scope(ctx, stream, KC_GEMM, 1);
-  FP4_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, w, x, sw, sx, args));
-  return FP4_OK;
+  return mx_launch<kernel>(dim3(unsigned(tiles * args.splits)), args.nt <= 32 ? FEW_THREADS - 128 : FEW_THREADS, smem, args.splits, stream, w, x, sw, sx, args);
 }
 
 }  // namespace

@@ -10,18 +10,25 @@
 //
 // All kernels walk the tensor in tiles of 128 x 128 elements, one block of 256 threads each: 128 elements are the scale tile's
 // four blocks of 32 (two tiles of blocks of 16) along either side, so both directions' codes and scales of a tile belong to one
-// block, and leave as 64-byte pieces (codes) and whole 512-byte tiles (scales).  A lane holds eight neighbours of a row; the four
-// (two) lanes of a block agree on its amax by shuffles.  Blocks along the columns are read back from a copy of the tile in
-// shared memory, 32 rows of two neighbouring columns a thread.
+// block.  Tiles travel between global and shared memory by TMA (rows of 128 bytes, 128-byte swizzle), codes too; a matrix
+// whose rows lie off 16-byte boundaries is copied by the threads, neighbouring lanes neighbouring elements.  In shared memory a
+// thread takes 64 neighbours of one row (blocks along the rows) and then 32 rows of two neighbouring columns (blocks along
+// the columns); either way it holds whole blocks and no two threads have to agree on an amax, and either access touches
+// every bank once.
+//
+// What bounds it: 4 to 5 instructions per element and direction, next to the bytes.  (A first version kept the tile in
+// registers, eight neighbours a lane, and found a block's amax by shuffles: 23 instructions for both directions, 75 % of the issue slots
+// at 40 % of the DRAM's throughput.)
+#include <cuda.h>
 #include <cuda_fp16.h>
 
 #include "mx.cuh"
+#include "tc_ptx.cuh"
 
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int WARP_ROWS = MX_TILE / (THREADS / 32);      // rows of a warp
-constexpr int STEPS = WARP_ROWS / 2;                     // it takes two at a time, 16 lanes each
+constexpr int BOX_BYTES = MX_TILE * 128;                 // 128 rows of 128 bytes
 
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
@@ -42,17 +49,18 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
 }
 
 // ------------------------------------------------------------------------- element types ---
-// Eight neighbours of a row as they lie in memory.
-template <class T>
-struct Vec8 {
-  static constexpr int WORDS = int(sizeof(T)) * 2;
-  uint32_t w[WORDS];
-};
+// `most(m, w)`: the larger magnitude in each half (of fp32: of the word), a NaN if either is one; the sign bits mean nothing.
 template <class T> struct TypeOf;
 template <> struct TypeOf<__nv_bfloat16> {
   static constexpr uint32_t INF = 0x7F80;
+  __device__ static uint32_t most(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
   __device__ static float value(uint32_t bits) { return __uint_as_float(bits << 16); }
-  __device__ static f32x2 pair(uint32_t w) { return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+  __device__ static float lo(uint32_t w) { return __uint_as_float(w << 16); }
+  __device__ static float hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
   __device__ static uint32_t word(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -60,113 +68,75 @@ template <> struct TypeOf<__nv_bfloat16> {
 };
 template <> struct TypeOf<__half> {
   static constexpr uint32_t INF = 0x7C00;
-  __device__ static float value(uint32_t bits) { return __half2float(__ushort_as_half(static_cast<unsigned short>(bits))); }
-  __device__ static f32x2 pair(uint32_t w) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    return pack2(f.x, f.y);
+  __device__ static uint32_t most(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
   }
+  __device__ static float value(uint32_t bits) { return __half2float(__ushort_as_half(static_cast<unsigned short>(bits))); }
+  __device__ static float lo(uint32_t w) { return __low2float(*reinterpret_cast<const __half2*>(&w)); }
+  __device__ static float hi(uint32_t w) { return __high2float(*reinterpret_cast<const __half2*>(&w)); }
   __device__ static uint32_t word(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
 };
-template <> struct TypeOf<float> { static constexpr uint32_t INF = 0x7F800000; };
-
-template <class T>
-__device__ __forceinline__ f32x2 pair_of(const Vec8<T>& v, int i) {       // elements 2 i and 2 i + 1
-  if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(v.w[2 * i]), __uint_as_float(v.w[2 * i + 1]));
-  else return TypeOf<T>::pair(v.w[i]);
-}
-template <class T>
-__device__ __forceinline__ void set_pair(Vec8<T>& v, int i, float a, float b) {
-  if constexpr (sizeof(T) == 4) { v.w[2 * i] = __float_as_uint(a); v.w[2 * i + 1] = __float_as_uint(b); }
-  else v.w[i] = TypeOf<T>::word(a, b);
-}
-// Bit patterns of magnitudes grow with the magnitude, and those of infinities and NaNs lie above all others: maxima are taken
-// over patterns, pairs of 16-bit types at a time.
-template <class T>
-__device__ __forceinline__ uint32_t max_patterns(uint32_t a, uint32_t b) {
-  if constexpr (sizeof(T) == 4) return max(a, b & 0x7FFFFFFFu);
-  else return __vmaxu2(a, b & 0x7FFF7FFFu);
-}
-template <class T>
-__device__ __forceinline__ uint32_t amax_word(const Vec8<T>& v) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < Vec8<T>::WORDS; ++i) m = max_patterns<T>(m, v.w[i]);
-  return m;
-}
-template <class T>
-__device__ __forceinline__ uint32_t join_halves(uint32_t m) {             // pattern of the larger half
-  if constexpr (sizeof(T) == 4) return m;
-  else return max(m & 0xFFFFu, m >> 16);
-}
-template <class T>
-__device__ __forceinline__ float pattern_value(uint32_t m) {
-  if constexpr (sizeof(T) == 4) return __uint_as_float(m);
-  else return TypeOf<T>::value(m);
-}
-
-// `wide`: the matrix's rows all start on 16-byte boundaries.
-template <class T>
-__device__ __forceinline__ Vec8<T> load8(const void* base, int64_t ld, int64_t row, int64_t col, int64_t cols, bool wide) {
-  Vec8<T> v;
-  const T* p = static_cast<const T*>(base) + row * ld + col;
-  if (wide && col + 8 <= cols) {
-#pragma unroll
-    for (int i = 0; i < Vec8<T>::WORDS / 4; ++i) {
-      const uint4 q = __ldg(reinterpret_cast<const uint4*>(p) + i);
-      v.w[4 * i] = q.x; v.w[4 * i + 1] = q.y; v.w[4 * i + 2] = q.z; v.w[4 * i + 3] = q.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint32_t bits = 0;
-      if (col + i < cols) {
-        if constexpr (sizeof(T) == 4) bits = __ldg(reinterpret_cast<const uint32_t*>(p) + i);
-        else bits = __ldg(reinterpret_cast<const unsigned short*>(p) + i);
-      }
-      if constexpr (sizeof(T) == 4) v.w[i] = bits;
-      else v.w[i / 2] = i % 2 ? v.w[i / 2] | (bits << 16) : bits;
-    }
+template <> struct TypeOf<float> {
+  static constexpr uint32_t INF = 0x7F800000;
+  __device__ static uint32_t most(uint32_t a, uint32_t b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(__uint_as_float(a))), "f"(fabsf(__uint_as_float(b))));
+    return __float_as_uint(r);
   }
-  return v;
-}
+  __device__ static float value(uint32_t bits) { return __uint_as_float(bits); }
+};
+// 32 neighbours of a row.
 template <class T>
-__device__ __forceinline__ void store8(void* base, int64_t ld, int64_t row, int64_t col, int64_t cols, bool wide, const Vec8<T>& v) {
-  T* p = static_cast<T*>(base) + row * ld + col;
-  if (wide && col + 8 <= cols) {
-#pragma unroll
-    for (int i = 0; i < Vec8<T>::WORDS / 4; ++i)
-      reinterpret_cast<uint4*>(p)[i] = make_uint4(v.w[4 * i], v.w[4 * i + 1], v.w[4 * i + 2], v.w[4 * i + 3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (col + i < cols) {
-        if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(p)[i] = v.w[i];
-        else reinterpret_cast<unsigned short*>(p)[i] = static_cast<unsigned short>(i % 2 ? v.w[i / 2] >> 16 : v.w[i / 2]);
-      }
+struct Run {
+  static constexpr int WORDS = 8 * int(sizeof(T));
+  uint32_t w[WORDS];
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return i % 2 ? TypeOf<T>::hi(w[i / 2]) : TypeOf<T>::lo(w[i / 2]);
   }
-}
+  __device__ __forceinline__ f32x2 pair(int i) const { return pack2(get(2 * i), get(2 * i + 1)); }
+  __device__ __forceinline__ void set_pair(int i, float a, float b) {
+    if constexpr (sizeof(T) == 4) { w[2 * i] = __float_as_uint(a); w[2 * i + 1] = __float_as_uint(b); }
+    else w[i] = TypeOf<T>::word(a, b);
+  }
+  // pattern of the largest magnitude of elements [first, first + n)
+  __device__ __forceinline__ uint32_t amax(int first, int n) const {
+    constexpr int PER = 4 / int(sizeof(T));
+    uint32_t m = w[first / PER];
+#pragma unroll
+    for (int i = 1; i < n / PER; ++i) m = TypeOf<T>::most(m, w[first / PER + i]);
+    if constexpr (sizeof(T) == 4) return m & 0x7FFFFFFFu;
+    else return max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+  }
+};
 
 // -------------------------------------------------------------------------------- codes ----
-__device__ __forceinline__ uint32_t e2m1_pair(f32x2 v) {                  // element 0 in the low nibble
-  float a, b;
-  unpack2(v, a, b);
+__device__ __forceinline__ uint32_t e2m1_word(const f32x2 (&v)[4]) {      // eight elements, the first in the low nibble
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
   uint32_t r;
-  asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(r) : "f"(a), "f"(b));
-  return r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r) : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
+  // nibbles 1000 become 0000: the sum has a nibble's top bit set where its magnitude is not 0
+  return r & (((r & 0x77777777u) + 0x77777777u) | 0x77777777u);
 }
-__device__ __forceinline__ uint32_t e4m3_pair(f32x2 v) {                  // element 0 in the low byte
-  float a, b;
-  unpack2(v, a, b);
-  unsigned short r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(r) : "f"(a), "f"(b));
+__device__ __forceinline__ uint32_t e4m3_word(f32x2 v0, f32x2 v1) {       // four elements, the first in the low byte
+  float a, b, c, d;
+  unpack2(v0, a, b);
+  unpack2(v1, c, d);
+  uint32_t r;
+  asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\tmov.b32 %0, {x, y};\n\t}"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
-}
-// Nibbles 1000 become 0000: the sum has a nibble's top bit set where its magnitude is not 0.
-__device__ __forceinline__ uint32_t clear_negative_zeros(uint32_t w) {
-  return w & (((w & 0x77777777u) + 0x77777777u) | 0x77777777u);
 }
 __device__ __forceinline__ float e4m3_value(uint32_t byte) {              // finite
   uint32_t h;
@@ -186,26 +156,26 @@ struct Scale {
 template <class T, int FMT>
 __device__ __forceinline__ Scale scale_of(uint32_t amax_pattern, float inv_tensor) {
   Scale r;
-  r.finite = amax_pattern < TypeOf<T>::INF;
-  const float amax = pattern_value<T>(amax_pattern);
+  r.finite = amax_pattern < TypeOf<T>::INF;                 // patterns of infinities and NaNs lie above all others
+  const float amax = TypeOf<T>::value(amax_pattern);
   if constexpr (FMT == FP4_MX_NVFP4) {
     // The quotient by 6, and later those by s, rounded correctly from the correctly rounded reciprocal (Markstein 1990:
     // q + (a - q s) inv in two fused steps); a value that lies on a tie of the format then comes out on it.
     const float a = amax * inv_tensor, sixth = 1.0f / 6.0f;
     const float q = a * sixth;
     const float v = fmaf(fmaf(-q, 6.0f, a), sixth, q);
-    r.byte = e4m3_pair(pack2(v, 0.0f)) & 0xFFu;
+    r.byte = e4m3_word(pack2(v, 0.0f), pack2(0.0f, 0.0f)) & 0xFFu;
     r.s = e4m3_value(r.byte);
     r.inv = r.byte ? __frcp_rn(r.s) : 0.0f;
     r.mul = inv_tensor;
-    if (!r.finite) { r.byte = 0x7Fu; r.mul = r.inv = r.s = 0.0f; }
+    if (!r.finite) r.byte = 0x7Fu;
   } else {
     // 6 = 1.5 * 2^2 and 448 = 1.75 * 2^8: the sum carries into the exponent where the mantissa is larger
     const uint32_t over = FMT == FP4_MX_E2M1 ? 0x7FFFFFu - 0x400000u : 0x7FFFFFu - 0x600000u;
     const int e8 = max(0, int((__float_as_uint(amax) + over) >> 23) - (FMT == FP4_MX_E2M1 ? 2 : 8));
     r.byte = uint32_t(e8);
     r.mul = __uint_as_float(uint32_t(254 - e8) << 23);
-    if (!r.finite) { r.byte = 0xFFu; r.mul = 0.0f; }
+    if (!r.finite) r.byte = 0xFFu;
   }
   return r;
 }
@@ -217,124 +187,187 @@ __device__ __forceinline__ f32x2 scaled(f32x2 x, const Scale& s) {
   const f32x2 q = mul2(v, inv);
   return fma2(fma2(q, neg, v), inv, q);
 }
-// Codes of eight elements: one word of nibbles or two of bytes.  (A block with an infinity or a NaN: 0.)
-template <class T, int FMT>
-__device__ __forceinline__ void encode8(const Vec8<T>& v, const Scale& s, uint32_t (&out)[FMT == FP4_MX_E4M3 ? 2 : 1]) {
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = FMT == FP4_MX_E4M3 ? e4m3_pair(scaled<FMT>(pair_of(v, i), s)) : e2m1_pair(scaled<FMT>(pair_of(v, i), s));
+// Codes of one block of N elements, pair(i) being elements 2 i and 2 i + 1.  (A block with an infinity or a NaN: 0.)
+template <int FMT, int N, class Pair>
+__device__ __forceinline__ void encode_block(const Scale& s, Pair pair, uint32_t* out) {
   if constexpr (FMT == FP4_MX_E4M3) {
-    out[0] = s.finite ? __byte_perm(r[0], r[1], 0x5410) : 0u;
-    out[1] = s.finite ? __byte_perm(r[2], r[3], 0x5410) : 0u;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) out[i] = e4m3_word(scaled<FMT>(pair(2 * i), s), scaled<FMT>(pair(2 * i + 1), s));
   } else {
-    const uint32_t w = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
-    out[0] = s.finite ? clear_negative_zeros(w) : 0u;
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+      const f32x2 v[4] = {scaled<FMT>(pair(4 * i), s), scaled<FMT>(pair(4 * i + 1), s), scaled<FMT>(pair(4 * i + 2), s), scaled<FMT>(pair(4 * i + 3), s)};
+      out[i] = e2m1_word(v);
+    }
   }
+  if (!s.finite)
+#pragma unroll
+    for (int i = 0; i < N / (FMT == FP4_MX_E4M3 ? 4 : 8); ++i) out[i] = 0;
+}
+__host__ __device__ constexpr int code_words(int fmt) { return fmt == FP4_MX_E4M3 ? 8 : 4; }               // of 32 elements
+__host__ __device__ constexpr int code_row_bytes(int fmt) { return fmt == FP4_MX_E4M3 ? 128 : 64; }        // of 128 elements
+
+// ------------------------------------------------------------------------ tiles in shared memory ---
+// A tile of T: boxes of 128 rows x 128 bytes, 16-byte unit u of row r at u ^ (r & 7).
+template <class T> __host__ __device__ constexpr int tile_bytes() { return MX_TILE * MX_TILE * int(sizeof(T)); }
+__device__ __forceinline__ uint32_t at128(int row, int byte) {                          // byte offset in a row of the tile
+  return uint32_t((byte >> 7) * BOX_BYTES + row * 128 + ((byte & 127) ^ ((row & 7) << 4)));
+}
+// 64-byte rows (codes in E2M1), 64-byte swizzle: unit u of row r at u ^ ((r >> 1) & 3).
+__device__ __forceinline__ uint32_t at64(int row, int byte) { return uint32_t(row * 64 + (byte ^ (((row >> 1) & 3) << 4))); }
+
+template <class T>
+__device__ __forceinline__ Run<T> load_run(const uint8_t* tile, int row, int run) {      // elements 32 run .. 32 run + 31
+  Run<T> v;
+#pragma unroll
+  for (int i = 0; i < Run<T>::WORDS / 4; ++i) {
+    const uint4 q = *reinterpret_cast<const uint4*>(tile + at128(row, run * 32 * int(sizeof(T)) + 16 * i));
+    v.w[4 * i] = q.x; v.w[4 * i + 1] = q.y; v.w[4 * i + 2] = q.z; v.w[4 * i + 3] = q.w;
+  }
+  return v;
+}
+// The 32 E4M3 codes of a run.
+struct Run8 {
+  uint32_t w[8];
+};
+__device__ __forceinline__ Run8 load_run8(const uint8_t* codes, int row, int run) {
+  const uint4 a = *reinterpret_cast<const uint4*>(codes + at128(row, run * 32)), b = *reinterpret_cast<const uint4*>(codes + at128(row, run * 32 + 16));
+  return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+template <class T>
+__device__ __forceinline__ void store_run(uint8_t* tile, int row, int run, const Run<T>& v) {
+#pragma unroll
+  for (int i = 0; i < Run<T>::WORDS / 4; ++i)
+    *reinterpret_cast<uint4*>(tile + at128(row, run * 32 * int(sizeof(T)) + 16 * i)) =
+        make_uint4(v.w[4 * i], v.w[4 * i + 1], v.w[4 * i + 2], v.w[4 * i + 3]);
 }
 
 // Where the scale byte of row r (0..127), block b of the tile of 128 elements goes among the tile's bytes.
 __device__ __forceinline__ int scale_at(int r, int b) { return (b >> 2) * 512 + (r & 31) * 16 + (r >> 5) * 4 + (b & 3); }
 __host__ __device__ constexpr int scale_tile_bytes(int fmt) { return fmt == FP4_MX_NVFP4 ? 1024 : 512; }
 
-// What the kernels write of one direction.
-struct Codes {
-  uint8_t* codes;
-  uint8_t* scales;
-  int64_t pitch;               // bytes of a row of codes
-  int64_t tiles;               // 128-element tiles of a row
+// Codes of a run of 32 elements into the staged codes of the tile (row r of 64 or 128 bytes), its scales among the tile's.
+template <class T, int FMT, class Pair, class Amax>
+__device__ __forceinline__ void encode_run(int r, int run, float inv_tensor, Pair pair, Amax amax, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+  constexpr int N = mx_block(FMT), BLOCKS = 32 / N;
+  uint32_t w[code_words(FMT)];
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b) {
+    const Scale s = scale_of<T, FMT>(amax(b * N, N), inv_tensor);
+    bad |= !s.finite;
+    s_scale[scale_at(r, run * BLOCKS + b)] = uint8_t(s.byte);
+    encode_block<FMT, N>(s, [&](int i) { return pair(b * (N / 2) + i); }, w + b * (code_words(FMT) / BLOCKS));
+  }
+  if constexpr (FMT == FP4_MX_E4M3) {
+    *reinterpret_cast<uint4*>(s_codes + at128(r, run * 32)) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(s_codes + at128(r, run * 32 + 16)) = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+    *reinterpret_cast<uint4*>(s_codes + at64(r, run * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// Blocks along the rows: the thread's run.
+template <class T, int FMT>
+__device__ __forceinline__ void encode_along(const Run<T>& v, int r, int run, float inv_tensor, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+  encode_run<T, FMT>(r, run, inv_tensor, [&](int i) { return v.pair(i); }, [&](int first, int n) { return v.amax(first, n); }, s_codes, s_scale, bad);
+}
+// Blocks along the columns: thread t takes columns 2 p and 2 p + 1 (p = t % 64) of rows 32 b .. 32 b + 31 (b = t / 64).  Row `column`
+// of the staged codes holds a column's.
+template <class T, int FMT>
+__device__ __forceinline__ void encode_across(const uint8_t* tile, float inv_tensor, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+  const int p = threadIdx.x & 63, b = threadIdx.x >> 6;
+  uint32_t a[32], c[sizeof(T) == 4 ? 32 : 1];              // 16 bits: both columns in a
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint8_t* q = tile + at128(32 * b + i, 2 * p * int(sizeof(T)));
+    if constexpr (sizeof(T) == 4) {
+      const uint2 w = *reinterpret_cast<const uint2*>(q);
+      a[i] = w.x; c[i] = w.y;
+    } else {
+      a[i] = *reinterpret_cast<const uint32_t*>(q);
+    }
+  }
+  // the largest magnitudes of both columns, of rows [16 h, 16 h + 16)
+  uint32_t ma[2], mc[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    ma[h] = a[16 * h];
+    if constexpr (sizeof(T) == 4) mc[h] = c[16 * h];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+      ma[h] = TypeOf<T>::most(ma[h], a[16 * h + i]);
+      if constexpr (sizeof(T) == 4) mc[h] = TypeOf<T>::most(mc[h], c[16 * h + i]);
+    }
+    if constexpr (sizeof(T) == 4) { ma[h] &= 0x7FFFFFFFu; mc[h] &= 0x7FFFFFFFu; }
+    else { mc[h] = (ma[h] >> 16) & 0x7FFFu; ma[h] &= 0x7FFFu; }
+  }
+#pragma unroll
+  for (int col = 0; col < 2; ++col) {
+    const auto value = [&](int i) {
+      if constexpr (sizeof(T) == 4) return __uint_as_float(col ? c[i] : a[i]);
+      else return col ? TypeOf<T>::hi(a[i]) : TypeOf<T>::lo(a[i]);
+    };
+    const uint32_t m0 = col ? mc[0] : ma[0], m1 = col ? mc[1] : ma[1];
+    encode_run<T, FMT>(2 * p + col, b, inv_tensor, [&](int i) { return pack2(value(2 * i), value(2 * i + 1)); },
+                       [&](int first, int n) { return n == 32 ? max(m0, m1) : first ? m1 : m0; }, s_codes, s_scale, bad);
+  }
+}
+
+// ------------------------------------------------------------------------ global <-> shared ---
+// One matrix or one tensor's codes as a kernel sees it.
+struct Side {
+  CUtensorMap map;             // boxes of 128 rows x 128 bytes (codes in E2M1: 64)
+  void* p;
+  int64_t ld;                  // elements
+  bool wide;                   // the map is there; else the threads copy
 };
-__device__ __forceinline__ void copy_out_scales(const uint8_t* smem, const Codes& c, int64_t row_tile, int64_t col_tile, int bytes) {
-  uint32_t* dst = reinterpret_cast<uint32_t*>(c.scales + (row_tile * c.tiles + col_tile) * bytes);
-  for (int i = threadIdx.x; i < bytes / 4; i += THREADS) dst[i] = reinterpret_cast<const uint32_t*>(smem)[i];
-}
-
-// Row `r` of the tile, eight elements of lane (lane & 15): the codes go out, the scale byte to shared memory.  All lanes call.
-template <class T, int FMT>
-__device__ __forceinline__ void encode_rows(const Vec8<T>& v, int r, int lane, bool row_there, int64_t row, int64_t col_tile,
-                                            float inv_tensor, const Codes& out, uint8_t* s_scale, bool& bad) {
-  uint32_t m = amax_word(v);
-  m = max_patterns<T>(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-  if (mx_block(FMT) == 32) m = max_patterns<T>(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-  const Scale s = scale_of<T, FMT>(join_halves<T>(m), inv_tensor);
-  bad |= !s.finite;
-  uint32_t w[FMT == FP4_MX_E4M3 ? 2 : 1];
-  encode8<T, FMT>(v, s, w);
-  const int piece = lane & 15;
-  if (piece % (mx_block(FMT) / 8) == 0) s_scale[scale_at(r, piece / (mx_block(FMT) / 8))] = uint8_t(s.byte);
-  if (row_there) {
-    uint8_t* p = out.codes + row * out.pitch + col_tile * (FMT == FP4_MX_E4M3 ? 128 : 64);
-    if constexpr (FMT == FP4_MX_E4M3) reinterpret_cast<uint2*>(p)[piece] = make_uint2(w[0], w[1]);
-    else reinterpret_cast<uint32_t*>(p)[piece] = w[0];
-  }
-}
-
-// The tile in shared memory: row r's 16-byte units, exchanged so that a thread's 32 rows and its neighbours' lie in other banks
-// (lanes of a quarter read the same two columns of rows 32 apart).
+// A tile's copies in and out.  The first call of the kernel's lives initialises the barrier.
+struct Loader {
+  uint64_t bar;
+  int abort;
+};
 template <class T>
-__device__ __forceinline__ void tile_store(uint8_t* tile, int r, int piece, const Vec8<T>& v) {
-  constexpr int ROW = MX_TILE * int(sizeof(T));
+__device__ __forceinline__ void request_tile(const Side& s, Loader* l, uint8_t* tile, int64_t row0, int64_t col0) {   // one thread
+  constexpr int PER = 128 / int(sizeof(T));
 #pragma unroll
-  for (int i = 0; i < Vec8<T>::WORDS / 4; ++i) {
-    const int unit = (piece * (Vec8<T>::WORDS / 4) + i) ^ ((r >> 5) << (sizeof(T) == 4 ? 2 : 1));
-    *reinterpret_cast<uint4*>(tile + r * ROW + unit * 16) = make_uint4(v.w[4 * i], v.w[4 * i + 1], v.w[4 * i + 2], v.w[4 * i + 3]);
+  for (int i = 0; i < tile_bytes<T>() / BOX_BYTES; ++i) tma_load_2d(tile + i * BOX_BYTES, &s.map, &l->bar, int(col0) + i * PER, int(row0));
+}
+template <class T>
+__device__ __forceinline__ void copy_tile_in(const Side& s, uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+  // 16 rows of a warp, 32 neighbouring elements at a time, eight such on their way together
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int i0 = 0; i0 < 64; i0 += 8) {
+    T v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t r = row0 + warp * 16 + ((i0 + j) >> 2), c = col0 + ((i0 + j) & 3) * 32 + lane;
+      if (r < rows && c < cols) v[j] = static_cast<const T*>(s.p)[r * s.ld + c];
+      else v[j] = T(0.0f);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<T*>(tile + at128(warp * 16 + ((i0 + j) >> 2), (((i0 + j) & 3) * 32 + lane) * int(sizeof(T)))) = v[j];
   }
 }
-// Blocks along the columns: thread t takes columns 2 p and 2 p + 1 (p = warp * 8 + lane / 4) of rows 32 b .. 32 b + 31
-// (b = lane % 4); four neighbouring lanes write 64 (E4M3: 128) contiguous bytes of a column's codes.
-template <class T, int FMT>
-__device__ __forceinline__ void encode_cols(const uint8_t* tile, int64_t row_tile, int64_t col_tile, int64_t cols,
-                                            float inv_tensor, const Codes& out, uint8_t* s_scale, bool& bad) {
-  constexpr int ROW = MX_TILE * int(sizeof(T)), N = mx_block(FMT);
-  const int lane = threadIdx.x & 31, p = (threadIdx.x >> 5) * 8 + (lane >> 2), b = lane & 3;
-#pragma unroll 1
-  for (int part = 0; part < 32 / N; ++part) {
-    uint32_t lo[N], hi[N];                   // fp32: the two columns; 16 bits: both in lo
-    uint32_t ma = 0, mb = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint8_t* row = tile + (32 * b + part * N + i) * ROW;
-      if constexpr (sizeof(T) == 4) {
-        const uint2 q = *reinterpret_cast<const uint2*>(row + ((p * 8) ^ (b << 6)));
-        lo[i] = q.x; hi[i] = q.y;
-        ma = max_patterns<T>(ma, q.x); mb = max_patterns<T>(mb, q.y);
-      } else {
-        lo[i] = *reinterpret_cast<const uint32_t*>(row + ((p * 4) ^ (b << 5)));
-        ma = max_patterns<T>(ma, lo[i]);
-      }
-    }
-    if constexpr (sizeof(T) == 2) { mb = ma >> 16; ma &= 0xFFFFu; }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const Scale s = scale_of<T, FMT>(c ? mb : ma, inv_tensor);
-      bad |= !s.finite;
-      const int col = 2 * p + c;
-      s_scale[scale_at(col, b * (32 / N) + part)] = uint8_t(s.byte);
-      uint32_t w[N / 8][FMT == FP4_MX_E4M3 ? 2 : 1];
-#pragma unroll
-      for (int k = 0; k < N / 8; ++k) {
-        Vec8<T> v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 8 * k + 2 * i;
-          if constexpr (sizeof(T) == 4) { v.w[2 * i] = c ? hi[e] : lo[e]; v.w[2 * i + 1] = c ? hi[e + 1] : lo[e + 1]; }
-          else v.w[i] = __byte_perm(lo[e], lo[e + 1], c ? 0x7632 : 0x5410);
-        }
-        encode8<T, FMT>(v, s, w[k]);
-      }
-      const int64_t gcol = col_tile * MX_TILE + col;
-      if (gcol < cols) {
-        if constexpr (FMT == FP4_MX_E4M3) {
-          uint4* dst = reinterpret_cast<uint4*>(out.codes + gcol * out.pitch + row_tile * 128 + b * 32);
-          dst[0] = make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
-          dst[1] = make_uint4(w[2][0], w[2][1], w[3][0], w[3][1]);
-        } else if constexpr (N == 32) {
-          *reinterpret_cast<uint4*>(out.codes + gcol * out.pitch + row_tile * 64 + b * 16) = make_uint4(w[0][0], w[1][0], w[2][0], w[3][0]);
-        } else {
-          *reinterpret_cast<uint2*>(out.codes + gcol * out.pitch + row_tile * 64 + b * 16 + part * 8) = make_uint2(w[0][0], w[1][0]);
-        }
-      }
-    }
+template <class T>
+__device__ __forceinline__ void copy_tile_out(const Side& s, const uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll 8
+  for (int i = 0; i < 64; ++i) {
+    const int64_t r = row0 + warp * 16 + (i >> 2), c = col0 + (i & 3) * 32 + lane;
+    if (r < rows && c < cols)
+      static_cast<T*>(s.p)[r * s.ld + c] = *reinterpret_cast<const T*>(tile + at128(warp * 16 + (i >> 2), ((i & 3) * 32 + lane) * int(sizeof(T))));
   }
+}
+template <class T>
+__device__ __forceinline__ void send_tile(const Side& s, const uint8_t* tile, int64_t row0, int64_t col0, int64_t cols) {   // one thread
+  constexpr int PER = 128 / int(sizeof(T));
+#pragma unroll
+  for (int i = 0; i < tile_bytes<T>() / BOX_BYTES; ++i)
+    if (col0 + i * PER < cols) tma_store_2d(&s.map, tile + i * BOX_BYTES, int(col0) + i * PER, int(row0));
+}
+__device__ __forceinline__ void copy_scales(uint8_t* dst, const uint8_t* smem, int bytes) {
+  for (int i = threadIdx.x; i < bytes / 4; i += THREADS) reinterpret_cast<uint32_t*>(dst)[i] = reinterpret_cast<const uint32_t*>(smem)[i];
 }
 
 struct TileAt {
@@ -345,99 +378,166 @@ __device__ __forceinline__ TileAt tile_at(int64_t col_tiles) {
   return {t / col_tiles, t % col_tiles};
 }
 __device__ __forceinline__ void report(bool bad, int32_t* status) {
-  if (__syncthreads_or(bad) && threadIdx.x == 0) atomicOr(status, FP4_DEV_NONFINITE);
+  if (__any_sync(0xFFFFFFFFu, bad) && (threadIdx.x & 31) == 0) atomicOr(status, FP4_DEV_NONFINITE);
 }
+
+// One direction of an operand as the kernels write it.
+struct Codes {
+  Side codes;
+  uint8_t* scales;
+  int64_t tiles;               // 128-element tiles of a row
+  bool on;
+};
 
 // -------------------------------------------------------------------------- quantisation ---
 struct QuantArgs {
-  const void* x;
-  int64_t rows, cols, ld;
-  bool wide;
-  Codes along, across;         // blocks along the rows, along the columns (codes null: not wanted)
+  Side x;
+  Codes along, across;         // blocks along the rows, along the columns
+  int64_t rows, cols;
   const uint32_t* amax;        // NVFP4
   int32_t* status;
 };
 template <class T, int FMT, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const QuantArgs a) {
-  extern __shared__ __align__(16) uint8_t tile[];
+__global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_constant__ QuantArgs a) {
+  constexpr int CODE_BYTES = MX_TILE * code_row_bytes(FMT);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* s_along = tile + tile_bytes<T>();
+  uint8_t* s_across = s_along + (ROWS ? CODE_BYTES : 0);
   __shared__ __align__(16) uint8_t s_scale[2][1024];
+  __shared__ Loader l;
   const TileAt at = tile_at(mx_tiles(a.cols));
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t col = at.col * MX_TILE + (lane & 15) * 8;
-  const float inv_tensor = FMT == FP4_MX_NVFP4 ? pow2_int(-mx_tensor_exponent(__ldg(a.amax))) : 1.0f;
-  bool bad = false;
-  Vec8<T> v[STEPS];
-#pragma unroll
-  for (int i = 0; i < STEPS; ++i) {
-    const int64_t row = at.row * MX_TILE + warp * WARP_ROWS + 2 * i + (lane >> 4);
-    if (row < a.rows && col < a.cols) v[i] = load8<T>(a.x, a.ld, row, col, a.cols, a.wide);
-    else
-#pragma unroll
-      for (int j = 0; j < Vec8<T>::WORDS; ++j) v[i].w[j] = 0;
+  const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
+  if (threadIdx.x == 0) {
+    mbar_init(&l.bar, 1);
+    l.abort = 0;
+    fence_async_smem();
   }
-#pragma unroll
-  for (int i = 0; i < STEPS; ++i) {
-    const int r = warp * WARP_ROWS + 2 * i + (lane >> 4);
-    const int64_t row = at.row * MX_TILE + r;
-    if (COLS) tile_store(tile, r, lane & 15, v[i]);
-    if (ROWS) encode_rows<T, FMT>(v[i], r, lane, row < a.rows, row, at.col, inv_tensor, a.along, s_scale[0], bad);
+  mx_wait_for_inputs();
+  mx_let_next_start();
+  if (a.x.wide) {
+    if (threadIdx.x == 0) {
+      mbar_arrive_expect_tx(&l.bar, tile_bytes<T>());
+      request_tile<T>(a.x, &l, tile, row0, col0);
+    }
+  } else {
+    copy_tile_in<T>(a.x, tile, row0, col0, a.rows, a.cols);
   }
+  const float inv_tensor = FMT == FP4_MX_NVFP4 ? pow2_int(-mx_tensor_exponent(*a.amax)) : 1.0f;
   __syncthreads();
-  if (COLS) {
-    encode_cols<T, FMT>(tile, at.row, at.col, a.cols, inv_tensor, a.across, s_scale[1], bad);
-    __syncthreads();
-    copy_out_scales(s_scale[1], a.across, at.col, at.row, scale_tile_bytes(FMT));
+  if (a.x.wide && !mbar_wait(&l.bar, 0, &l.abort, a.status)) return;      // (a copy that never comes: nothing is written)
+  bool bad = false;
+  if (ROWS) {
+    const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) encode_along<T, FMT>(load_run<T>(tile, r, run0 + i), r, run0 + i, inv_tensor, s_along, s_scale[0], bad);
   }
-  if (ROWS) copy_out_scales(s_scale[0], a.along, at.row, at.col, scale_tile_bytes(FMT));
+  if (COLS) encode_across<T, FMT>(tile, inv_tensor, s_across, s_scale[1], bad);
+  fence_async_smem();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (ROWS) tma_store_2d(&a.along.codes.map, s_along, int(at.col) * code_row_bytes(FMT), int(row0));
+    if (COLS) tma_store_2d(&a.across.codes.map, s_across, int(at.row) * code_row_bytes(FMT), int(col0));
+  }
+  constexpr int BYTES = scale_tile_bytes(FMT);
+  if (ROWS) copy_scales(a.along.scales + (at.row * a.along.tiles + at.col) * BYTES, s_scale[0], BYTES);
+  if (COLS) copy_scales(a.across.scales + (at.col * a.across.tiles + at.row) * BYTES, s_scale[1], BYTES);
   report(bad, a.status);
+  if (threadIdx.x == 0) tma_store_wait_all();
 }
 
-// Largest magnitude of a tensor as a pattern of fp32 (integer maxima: the order of the blocks does not matter).
+// Largest magnitude of a tensor as a pattern of fp32 (integer maxima: the order of the blocks does not matter).  `wide`: rows on 16-byte
+// boundaries; 16 bytes a lane, eight such on their way together.
+struct AmaxArgs {
+  const void* x;
+  int64_t rows, cols, ld;
+  bool wide;
+  uint32_t* amax;
+};
 template <class T>
-__global__ void __launch_bounds__(THREADS) mx_amax_kernel(const void* x, int64_t rows, int64_t cols, int64_t ld, bool wide, uint32_t* amax) {
-  const int64_t per_row = (cols + 7) / 8, n = rows * per_row, step = int64_t(gridDim.x) * THREADS;
+__global__ void __launch_bounds__(THREADS) mx_amax_kernel(const AmaxArgs a) {
+  mx_wait_for_inputs();
+  mx_let_next_start();
+  constexpr int PER = 16 / int(sizeof(T)), AT_ONCE = 8;
   uint32_t m = 0;
-  for (int64_t i = int64_t(blockIdx.x) * THREADS + threadIdx.x; i < n; i += 4 * step) {
-    Vec8<T> v[4];
+  const int lane = threadIdx.x & 31;
+  // a warp walks along rows, in pieces of 32 x AT_ONCE loads
+  const int64_t warps = int64_t(gridDim.x) * (THREADS / 32), warp = int64_t(blockIdx.x) * (THREADS / 32) + (threadIdx.x >> 5);
+  const int64_t piece = a.wide ? 32 * AT_ONCE * PER : 32 * AT_ONCE, pieces = (a.cols + piece - 1) / piece;
+  for (int64_t row = warp / pieces, p = warp % pieces; row < a.rows;) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ld;
+    const int64_t c0 = p * piece;
+    if (a.wide) {
+      uint4 q[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t k = i + j * step;
-      if (k < n) v[j] = load8<T>(x, ld, k / per_row, k % per_row * 8, cols, wide);
-      else
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int64_t c = c0 + (i * 32 + lane) * PER;
+        q[i] = make_uint4(0, 0, 0, 0);
+        if (c + PER <= a.cols) q[i] = __ldg(reinterpret_cast<const uint4*>(x + c));
+        else if (c < a.cols) {                             // the row's last, partial 16 bytes
+          uint32_t w[4] = {0, 0, 0, 0};
+          for (int j = 0; j < PER; ++j)
+            if (c + j < a.cols) {
+              if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(x[c + j]);
+              else w[j / 2] |= uint32_t(*reinterpret_cast<const unsigned short*>(x + c + j)) << (16 * (j & 1));
+            }
+          q[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
 #pragma unroll
-        for (int w = 0; w < Vec8<T>::WORDS; ++w) v[j].w[w] = 0;
+      for (int i = 0; i < AT_ONCE; ++i)
+        m = TypeOf<T>::most(m, TypeOf<T>::most(TypeOf<T>::most(q[i].x, q[i].y), TypeOf<T>::most(q[i].z, q[i].w)));
+    } else {
+      uint32_t v[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int64_t c = c0 + i * 32 + lane;
+        v[i] = 0;
+        if (c < a.cols) {
+          if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(x[c]);
+          else v[i] = *reinterpret_cast<const unsigned short*>(x + c);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) m = TypeOf<T>::most(m, v[i]);
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = max_patterns<T>(m, amax_word(v[j]));
+    p += warps;
+    if (p >= pieces) {
+      row += p / pieces;
+      p %= pieces;
+    }
   }
-  m = __reduce_max_sync(0xFFFFFFFFu, join_halves<T>(m));
+  if constexpr (sizeof(T) == 2) m = max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+  else m &= 0x7FFFFFFFu;
+  m = __reduce_max_sync(0xFFFFFFFFu, m);
   __shared__ uint32_t s[THREADS / 32];
-  if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = m;
+  if (lane == 0) s[threadIdx.x >> 5] = m;
   __syncthreads();
   if (threadIdx.x < 32) {
     m = __reduce_max_sync(0xFFFFFFFFu, threadIdx.x < THREADS / 32 ? s[threadIdx.x] : 0u);
-    if (threadIdx.x == 0 && m) atomicMax(amax, __float_as_uint(pattern_value<T>(m)));
+    if (threadIdx.x == 0 && m) atomicMax(a.amax, __float_as_uint(TypeOf<T>::value(m)));
   }
 }
 
 // ------------------------------------------------------------------------ dequantisation ---
-__device__ __forceinline__ void decode8_e4m3(uint2 w, float s, float (&f)[8]) {
+__device__ __forceinline__ void decode4_e4m3(uint32_t w, float s, float* f) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const unsigned short h = static_cast<unsigned short>((i < 2 ? w.x : w.y) >> (16 * (i & 1)));
+  for (int i = 0; i < 2; ++i) {
     uint32_t t;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(t) : "h"(h));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(t) : "h"(static_cast<unsigned short>(w >> (16 * i))));
     const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&t));
     f[2 * i] = v.x * s;
     f[2 * i + 1] = v.y * s;
   }
 }
-__device__ __forceinline__ void decode8_e2m1(uint32_t w, float s, float (&f)[8]) {
+__device__ __forceinline__ void decode8_e2m1(uint32_t w, float s, float* f) {
+  uint32_t t[4];
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(t[0]), "=r"(t[1]), "=r"(t[2]), "=r"(t[3]) : "r"(w));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t t;
-    asm("{\n\t.reg .b8 b;\n\tcvt.u8.u32 b, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(t) : "r"((w >> (8 * i)) & 0xFFu));
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&t));
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&t[i]));
     f[2 * i] = v.x * s;
     f[2 * i + 1] = v.y * s;
   }
@@ -448,60 +548,68 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
   if (FMT == FP4_MX_NVFP4) return byte == 0x7Fu ? __uint_as_float(0x7FC00000u) : e4m3_value(byte);
   return byte == 0xFFu ? __uint_as_float(0x7FC00000u) : pow2_byte(byte);
 }
-template <class T>
-__device__ __forceinline__ Vec8<T> vec_of(const float (&f)[8]) {
-  Vec8<T> v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) set_pair(v, i, f[2 * i], f[2 * i + 1]);
-  return v;
-}
 
 struct DequantArgs {
-  const uint8_t *codes, *scales;
+  Side codes, out;
+  const uint8_t* scales;
   const uint32_t* amax;
   int64_t rows, cols;
-  void* out;
-  int64_t ld;
-  bool wide;
+  int32_t* status;
 };
 template <class T, int FMT>
-__global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const DequantArgs a) {
-  constexpr int BYTES = scale_tile_bytes(FMT);
+__global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_constant__ DequantArgs a) {
+  constexpr int BYTES = scale_tile_bytes(FMT), CODE_BYTES = MX_TILE * code_row_bytes(FMT), N = mx_block(FMT);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* s_codes = tile + tile_bytes<T>();
   __shared__ __align__(16) uint8_t s_scale[BYTES];
+  __shared__ Loader l;
   const int64_t col_tiles = mx_tiles(a.cols);
   const TileAt at = tile_at(col_tiles);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane & 15;
-  const uint8_t* src = a.scales + (at.row * col_tiles + at.col) * BYTES;
-  for (int i = threadIdx.x; i < BYTES / 4; i += THREADS)
-    reinterpret_cast<uint32_t*>(s_scale)[i] = __ldg(reinterpret_cast<const uint32_t*>(src) + i);
-  const float tensor = FMT == FP4_MX_NVFP4 ? pow2_int(mx_tensor_exponent(__ldg(a.amax))) : 1.0f;
-  const int64_t pitch = mx_pitch(a.cols, FMT);
-  uint2 w[STEPS];
-#pragma unroll
-  for (int i = 0; i < STEPS; ++i) {
-    const int64_t row = at.row * MX_TILE + warp * WARP_ROWS + 2 * i + (lane >> 4);
-    w[i] = make_uint2(0, 0);
-    if (row < a.rows) {
-      const uint8_t* p = a.codes + row * pitch + at.col * (FMT == FP4_MX_E4M3 ? 128 : 64);
-      if (FMT == FP4_MX_E4M3) w[i] = __ldg(reinterpret_cast<const uint2*>(p) + piece);
-      else w[i].x = __ldg(reinterpret_cast<const uint32_t*>(p) + piece);
-    }
+  const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
+  if (threadIdx.x == 0) {
+    mbar_init(&l.bar, 1);
+    l.abort = 0;
+    fence_async_smem();
   }
+  mx_wait_for_inputs();
+  mx_let_next_start();
+  if (threadIdx.x == 0) {
+    mbar_arrive_expect_tx(&l.bar, CODE_BYTES);
+    tma_load_2d(s_codes, &a.codes.map, &l.bar, int(at.col) * code_row_bytes(FMT), int(row0));
+  }
+  copy_scales(s_scale, a.scales + (at.row * col_tiles + at.col) * BYTES, BYTES);
+  const float tensor = FMT == FP4_MX_NVFP4 ? pow2_int(mx_tensor_exponent(*a.amax)) : 1.0f;
   __syncthreads();
-  const int64_t col = at.col * MX_TILE + piece * 8;
+  if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
+  const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
 #pragma unroll
-  for (int i = 0; i < STEPS; ++i) {
-    const int r = warp * WARP_ROWS + 2 * i + (lane >> 4);
-    const int64_t row = at.row * MX_TILE + r;
+  for (int run = run0; run < run0 + 2; ++run) {
+    float f[32];
+    if constexpr (FMT == FP4_MX_E4M3) {
+      const float s = scale_value<FMT>(s_scale[scale_at(r, run)]);
+      const Run8 q = load_run8(s_codes, r, run);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) decode4_e4m3(q.w[i], s, f + 4 * i);
+    } else {
+      const uint4 q = *reinterpret_cast<const uint4*>(s_codes + at64(r, run * 16));
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) decode8_e2m1(w[i], scale_value<FMT>(s_scale[scale_at(r, (run * 32 + 8 * i) / N)]), f + 8 * i);
+    }
     // (a product of a code, its scale and the tensor's power of two is exact until the last step, which may round or overflow)
-    const float s = scale_value<FMT>(s_scale[scale_at(r, piece * 8 / mx_block(FMT))]);
-    float f[8];
-    if (FMT == FP4_MX_E4M3) decode8_e4m3(w[i], s, f);
-    else decode8_e2m1(w[i].x, s, f);
-    if (FMT == FP4_MX_NVFP4)
+    Run<T> v;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] *= tensor;
-    if (row < a.rows && col < a.cols) store8<T>(a.out, a.ld, row, col, a.cols, a.wide, vec_of<T>(f));
+    for (int i = 0; i < 16; ++i) v.set_pair(i, FMT == FP4_MX_NVFP4 ? f[2 * i] * tensor : f[2 * i], FMT == FP4_MX_NVFP4 ? f[2 * i + 1] * tensor : f[2 * i + 1]);
+    store_run(tile, r, run, v);
+  }
+  fence_async_smem();
+  __syncthreads();
+  if (!a.out.wide) {
+    copy_tile_out<T>(a.out, tile, row0, col0, a.rows, a.cols);
+  } else if (threadIdx.x == 0) {
+    send_tile<T>(a.out, tile, row0, col0, a.cols);
+    tma_store_wait_all();
   }
 }
 
@@ -517,267 +625,365 @@ __device__ __forceinline__ Sigmoid sigmoid(float g) {
 }
 
 struct SwigluArgs {
-  const void *gate, *up;       // forward
-  int64_t ld_gate, ld_up;
-  Codes ckpt_gate, ckpt_up;    // forward: written (codes null: not wanted); backward: read
-  const void* dh;              // backward
-  void *dgate, *dup;
-  int64_t ld_dh, ld_dgate, ld_dup;
-  void* h;                     // either (null: not wanted)
-  int64_t ld_h;
-  Codes along, across;
+  Side gate, up;               // forward: inputs; backward: d_gate and d_up
+  Side dh;                     // backward
+  Codes ckpt_gate, ckpt_up;    // forward: written; backward: read
+  Side h;
+  bool has_h;
+  Codes along, across;         // h as an operand
   int64_t rows, cols;
-  bool wide;                   // every matrix of the caller's has rows on 16-byte boundaries
   int32_t* status;
 };
-template <class T, bool BWD, bool KEEP, bool COLS>
-__global__ void __launch_bounds__(THREADS) mx_swiglu_kernel(const SwigluArgs a) {
-  extern __shared__ __align__(16) uint8_t tile[];
-  __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
-  const TileAt at = tile_at(mx_tiles(a.cols));
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, piece = lane & 15;
-  const int64_t col = at.col * MX_TILE + piece * 8;
-  bool bad = false;
-  if (BWD) {
-    const int64_t tile_no = (at.row * a.ckpt_gate.tiles + at.col) * 512;
-    if (threadIdx.x < 128)
-      reinterpret_cast<uint32_t*>(s_scale[2])[threadIdx.x] = __ldg(reinterpret_cast<const uint32_t*>(a.ckpt_gate.scales + tile_no) + threadIdx.x);
-    else
-      reinterpret_cast<uint32_t*>(s_scale[3])[threadIdx.x - 128] = __ldg(reinterpret_cast<const uint32_t*>(a.ckpt_up.scales + tile_no) + threadIdx.x - 128);
-    __syncthreads();
-  }
-  constexpr int AT_ONCE = 4;
-#pragma unroll 1
-  for (int i0 = 0; i0 < STEPS; i0 += AT_ONCE) {
-    Vec8<T> x[AT_ONCE], y[AT_ONCE];            // forward: gate and up; backward: dh
-    uint2 cg[AT_ONCE], cu[AT_ONCE];
-#pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const int64_t row = at.row * MX_TILE + warp * WARP_ROWS + 2 * (i0 + i) + (lane >> 4);
-      const bool there = row < a.rows && col < a.cols;
-#pragma unroll
-      for (int j = 0; j < Vec8<T>::WORDS; ++j) x[i].w[j] = y[i].w[j] = 0;
-      cg[i] = cu[i] = make_uint2(0, 0);
-      if (there) {
-        if (BWD) {
-          x[i] = load8<T>(a.dh, a.ld_dh, row, col, a.cols, a.wide);
-          cg[i] = __ldg(reinterpret_cast<const uint2*>(a.ckpt_gate.codes + row * a.ckpt_gate.pitch + at.col * 128) + piece);
-          cu[i] = __ldg(reinterpret_cast<const uint2*>(a.ckpt_up.codes + row * a.ckpt_up.pitch + at.col * 128) + piece);
-        } else {
-          x[i] = load8<T>(a.gate, a.ld_gate, row, col, a.cols, a.wide);
-          y[i] = load8<T>(a.up, a.ld_up, row, col, a.cols, a.wide);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const int r = warp * WARP_ROWS + 2 * (i0 + i) + (lane >> 4);
-      const int64_t row = at.row * MX_TILE + r;
-      const bool there = row < a.rows && col < a.cols;
-      float g[8], u[8], h[8];
-      if (BWD) {
-        decode8_e4m3(cg[i], scale_value<FP4_MX_E4M3>(s_scale[2][scale_at(r, piece / 4)]), g);
-        decode8_e4m3(cu[i], scale_value<FP4_MX_E4M3>(s_scale[3][scale_at(r, piece / 4)]), u);
-        float dg[8], du[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float d[2];
-          unpack2(pair_of(x[i], j), d[0], d[1]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int k = 2 * j + e;
-            const Sigmoid s = sigmoid(g[k]);
-            const float gs = g[k] * s.s;
-            h[k] = gs * u[k];
-            du[k] = d[e] * gs;
-            // d/dg g s = s (1 + g (1 - s)) = s + g s (1 - s)
-            dg[k] = d[e] * u[k] * fmaf(gs, s.rest, s.s);
-          }
-        }
-        if (there) {
-          store8<T>(a.dgate, a.ld_dgate, row, col, a.cols, a.wide, vec_of<T>(dg));
-          store8<T>(a.dup, a.ld_dup, row, col, a.cols, a.wide, vec_of<T>(du));
-        }
-        // (dh: no block of it is scaled here, so its infinities and NaNs pass on to the gradients as they are)
-      } else {
-        if (KEEP) {
-          encode_rows<T, FP4_MX_E4M3>(x[i], r, lane, row < a.rows, row, at.col, 1.0f, a.ckpt_gate, s_scale[2], bad);
-          encode_rows<T, FP4_MX_E4M3>(y[i], r, lane, row < a.rows, row, at.col, 1.0f, a.ckpt_up, s_scale[3], bad);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          unpack2(pair_of(x[i], j), g[2 * j], g[2 * j + 1]);
-          unpack2(pair_of(y[i], j), u[2 * j], u[2 * j + 1]);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) h[k] = g[k] * sigmoid(g[k]).s * u[k];
-      }
-      const Vec8<T> hv = vec_of<T>(h);
-      if (a.h && there) store8<T>(a.h, a.ld_h, row, col, a.cols, a.wide, hv);
-      if (a.along.codes) encode_rows<T, FP4_MX_E2M1>(hv, r, lane, row < a.rows, row, at.col, 1.0f, a.along, s_scale[0], bad);
-      if (COLS) tile_store(tile, r, piece, hv);
-    }
-  }
+// h (in `tile`, complete) as an operand and as a matrix.
+template <class T>
+__device__ __forceinline__ void finish_h(const SwigluArgs& a, const TileAt& at, uint8_t* tile, uint8_t* s_along, uint8_t* s_across,
+                                         uint8_t (*s_scale)[512], bool& bad) {
+  const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
+  if (a.across.on) encode_across<T, FP4_MX_E2M1>(tile, 1.0f, s_across, s_scale[1], bad);
+  fence_async_smem();
   __syncthreads();
-  if (COLS) {
-    encode_cols<T, FP4_MX_E2M1>(tile, at.row, at.col, a.cols, 1.0f, a.across, s_scale[1], bad);
-    __syncthreads();
-    copy_out_scales(s_scale[1], a.across, at.col, at.row, 512);
+  if (threadIdx.x == 0) {
+    if (a.has_h && a.h.wide) send_tile<T>(a.h, tile, row0, col0, a.cols);
+    if (a.along.on) tma_store_2d(&a.along.codes.map, s_along, int(at.col) * 64, int(row0));
+    if (a.across.on) tma_store_2d(&a.across.codes.map, s_across, int(at.row) * 64, int(col0));
   }
-  if (a.along.codes) copy_out_scales(s_scale[0], a.along, at.row, at.col, 512);
-  if (!BWD && KEEP) {
-    copy_out_scales(s_scale[2], a.ckpt_gate, at.row, at.col, 512);
-    copy_out_scales(s_scale[3], a.ckpt_up, at.row, at.col, 512);
+  if (a.has_h && !a.h.wide) copy_tile_out<T>(a.h, tile, row0, col0, a.rows, a.cols);
+  if (a.along.on) copy_scales(a.along.scales + (at.row * a.along.tiles + at.col) * 512, s_scale[0], 512);
+  if (a.across.on) copy_scales(a.across.scales + (at.col * a.across.tiles + at.row) * 512, s_scale[1], 512);
+}
+// Shared memory: gate (then h), up, and as they are wanted the checkpoints' codes and h's in either direction.
+template <class T, bool KEEP>
+__global__ void __launch_bounds__(THREADS) mx_swiglu_fwd_kernel(const __grid_constant__ SwigluArgs a) {
+  constexpr int CODES8 = MX_TILE * 128, CODES4 = MX_TILE * 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* t_up = tile + tile_bytes<T>();
+  uint8_t* s_gate = t_up + tile_bytes<T>();
+  uint8_t* s_up = s_gate + (KEEP ? CODES8 : 0);
+  uint8_t* s_along = s_up + (KEEP ? CODES8 : 0);
+  uint8_t* s_across = s_along + (a.along.on ? CODES4 : 0);
+  __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
+  __shared__ Loader l;
+  const TileAt at = tile_at(mx_tiles(a.cols));
+  const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
+  if (threadIdx.x == 0) {
+    mbar_init(&l.bar, 1);
+    l.abort = 0;
+    fence_async_smem();
+  }
+  mx_wait_for_inputs();
+  mx_let_next_start();
+  if (threadIdx.x == 0) {
+    mbar_arrive_expect_tx(&l.bar, (a.gate.wide ? tile_bytes<T>() : 0) + (a.up.wide ? tile_bytes<T>() : 0));
+    if (a.gate.wide) request_tile<T>(a.gate, &l, tile, row0, col0);
+    if (a.up.wide) request_tile<T>(a.up, &l, t_up, row0, col0);
+  }
+  if (!a.gate.wide) copy_tile_in<T>(a.gate, tile, row0, col0, a.rows, a.cols);
+  if (!a.up.wide) copy_tile_in<T>(a.up, t_up, row0, col0, a.rows, a.cols);
+  __syncthreads();
+  if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
+  bool bad = false;
+  const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
+#pragma unroll 1
+  for (int run = run0; run < run0 + 2; ++run) {
+    Run<T> g = load_run<T>(tile, r, run);
+    const Run<T> u = load_run<T>(t_up, r, run);
+    if (KEEP) {
+      encode_along<T, FP4_MX_E4M3>(g, r, run, 1.0f, s_gate, s_scale[2], bad);
+      encode_along<T, FP4_MX_E4M3>(u, r, run, 1.0f, s_up, s_scale[3], bad);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float g0 = g.get(2 * i), g1 = g.get(2 * i + 1);
+      g.set_pair(i, g0 * sigmoid(g0).s * u.get(2 * i), g1 * sigmoid(g1).s * u.get(2 * i + 1));
+    }
+    if (a.has_h || a.across.on) store_run(tile, r, run, g);
+    if (a.along.on) encode_along<T, FP4_MX_E2M1>(g, r, run, 1.0f, s_along, s_scale[0], bad);
+  }
+  if (a.across.on) __syncthreads();
+  finish_h<T>(a, at, tile, s_along, s_across, s_scale, bad);
+  if (KEEP) {
+    if (threadIdx.x == 0) {
+      tma_store_2d(&a.ckpt_gate.codes.map, s_gate, int(at.col) * 128, int(row0));
+      tma_store_2d(&a.ckpt_up.codes.map, s_up, int(at.col) * 128, int(row0));
+    }
+    copy_scales(a.ckpt_gate.scales + (at.row * a.ckpt_gate.tiles + at.col) * 512, s_scale[2], 512);
+    copy_scales(a.ckpt_up.scales + (at.row * a.ckpt_up.tiles + at.col) * 512, s_scale[3], 512);
   }
   report(bad, a.status);
+  if (threadIdx.x == 0) tma_store_wait_all();
+}
+// Shared memory: dh (then d_gate), d_up (then h), the checkpoints' codes, and h's as they are wanted.  h is made behind the gradients, once
+// their copies have read the tile that it takes: a tile of its own would leave one block an SM.
+template <class T, bool H>
+__global__ void __launch_bounds__(THREADS) mx_swiglu_bwd_kernel(const __grid_constant__ SwigluArgs a) {
+  constexpr int CODES8 = MX_TILE * 128, CODES4 = MX_TILE * 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* t_up = tile + tile_bytes<T>();
+  uint8_t* s_gate = t_up + tile_bytes<T>();
+  uint8_t* s_up = s_gate + CODES8;
+  uint8_t* s_along = s_up + CODES8;
+  uint8_t* s_across = s_along + (H && a.along.on ? CODES4 : 0);
+  __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
+  __shared__ Loader l;
+  const TileAt at = tile_at(mx_tiles(a.cols));
+  const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
+  if (threadIdx.x == 0) {
+    mbar_init(&l.bar, 1);
+    l.abort = 0;
+    fence_async_smem();
+  }
+  mx_wait_for_inputs();
+  mx_let_next_start();
+  if (threadIdx.x == 0) {
+    mbar_arrive_expect_tx(&l.bar, 2 * CODES8 + (a.dh.wide ? tile_bytes<T>() : 0));
+    tma_load_2d(s_gate, &a.ckpt_gate.codes.map, &l.bar, int(at.col) * 128, int(row0));
+    tma_load_2d(s_up, &a.ckpt_up.codes.map, &l.bar, int(at.col) * 128, int(row0));
+    if (a.dh.wide) request_tile<T>(a.dh, &l, tile, row0, col0);
+  }
+  if (!a.dh.wide) copy_tile_in<T>(a.dh, tile, row0, col0, a.rows, a.cols);
+  copy_scales(s_scale[2], a.ckpt_gate.scales + (at.row * a.ckpt_gate.tiles + at.col) * 512, 512);
+  copy_scales(s_scale[3], a.ckpt_up.scales + (at.row * a.ckpt_up.tiles + at.col) * 512, 512);
+  __syncthreads();
+  if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
+  const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
+#pragma unroll 1
+  for (int run = run0; run < run0 + 2; ++run) {
+    const float sg = scale_value<FP4_MX_E4M3>(s_scale[2][scale_at(r, run)]), su = scale_value<FP4_MX_E4M3>(s_scale[3][scale_at(r, run)]);
+    const Run8 cg = load_run8(s_gate, r, run), cu = load_run8(s_up, r, run);
+    Run<T> d = load_run<T>(tile, r, run), e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float g[4], u[4], dg[4], du[4];
+      decode4_e4m3(cg.w[i], sg, g);
+      decode4_e4m3(cu.w[i], su, u);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const Sigmoid s = sigmoid(g[k]);
+        const float gs = g[k] * s.s, dh = d.get(4 * i + k);
+        du[k] = dh * gs;
+        dg[k] = dh * u[k] * fmaf(gs, s.rest, s.s);         // d/dg g s = s (1 + g (1 - s)) = s + g s (1 - s)
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        d.set_pair(2 * i + k, dg[2 * k], dg[2 * k + 1]);
+        e.set_pair(2 * i + k, du[2 * k], du[2 * k + 1]);
+      }
+    }
+    store_run(tile, r, run, d);
+    store_run(t_up, r, run, e);
+  }
+  fence_async_smem();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (a.up.wide) send_tile<T>(a.up, t_up, row0, col0, a.cols);
+    if (a.gate.wide) send_tile<T>(a.gate, tile, row0, col0, a.cols);
+  }
+  if (!a.up.wide) copy_tile_out<T>(a.up, t_up, row0, col0, a.rows, a.cols);
+  if (!a.gate.wide) copy_tile_out<T>(a.gate, tile, row0, col0, a.rows, a.cols);
+  if (H) {
+    if (threadIdx.x == 0) tma_store_wait_read_0();
+    __syncthreads();
+    bool bad = false;
+#pragma unroll 1
+    for (int run = run0; run < run0 + 2; ++run) {
+      const float sg = scale_value<FP4_MX_E4M3>(s_scale[2][scale_at(r, run)]), su = scale_value<FP4_MX_E4M3>(s_scale[3][scale_at(r, run)]);
+      const Run8 cg = load_run8(s_gate, r, run), cu = load_run8(s_up, r, run);
+      Run<T> v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float g[4], u[4];
+        decode4_e4m3(cg.w[i], sg, g);
+      decode4_e4m3(cu.w[i], su, u);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          v.set_pair(2 * i + k, g[2 * k] * sigmoid(g[2 * k]).s * u[2 * k], g[2 * k + 1] * sigmoid(g[2 * k + 1]).s * u[2 * k + 1]);
+      }
+      store_run(t_up, r, run, v);
+      if (a.along.on) encode_along<T, FP4_MX_E2M1>(v, r, run, 1.0f, s_along, s_scale[0], bad);
+    }
+    if (a.across.on) __syncthreads();
+    finish_h<T>(a, at, t_up, s_along, s_across, s_scale, bad);
+    report(bad, a.status);
+  }
+  if (threadIdx.x == 0) tma_store_wait_all();
 }
 
 // ------------------------------------------------------------------------------ launches ---
-bool rows_aligned(const void* p, int64_t ld, int dtype) {
-  const int64_t elt = dtype == FP4_DTYPE_FP32 ? 4 : 2;
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * elt) % 16 == 0;
+int elt_bytes(int dtype) { return dtype == FP4_DTYPE_FP32 ? 4 : 2; }
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+int make_map(fp4_ctx* ctx, CUtensorMap* map, CUtensorMapDataType type, const void* p, int64_t inner, int64_t outer, int64_t stride_bytes, int box_inner,
+             CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[2] = {cuuint64_t(inner), cuuint64_t(outer)}, strides[1] = {cuuint64_t(stride_bytes)};
+  const cuuint32_t box[2] = {cuuint32_t(box_inner), MX_TILE}, elem_strides[2] = {1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(map, type, 2, const_cast<void*>(p), dims, strides, box, elem_strides,
+                                                                        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? FP4_OK : FP4_ERR_CUDA;
 }
-Codes codes_along(const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
-  (void)rows;
-  return {q.codes, q.scales, mx_pitch(cols, q.format), mx_tiles(cols)};
+// A matrix: by TMA where its rows lie on 16-byte boundaries (one that is written: end there too, since a bulk store clips to whole
+// 16 bytes).
+int matrix_side(fp4_ctx* ctx, Side* s, MxMatrix m, int64_t rows, int64_t cols, int dtype, bool written) {
+  const int elt = elt_bytes(dtype);
+  s->p = const_cast<void*>(m.p);
+  s->ld = m.ld;
+  s->wide = (reinterpret_cast<uintptr_t>(m.p) & 15) == 0 && (m.ld * elt) % 16 == 0 && (!written || (cols * elt) % 16 == 0);
+  if (!s->wide) return FP4_OK;
+  const CUtensorMapDataType type = dtype == FP4_DTYPE_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == FP4_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                             : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return make_map(ctx, &s->map, type, m.p, cols, rows, m.ld * elt, 128 / elt, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-Codes codes_across(const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
-  (void)cols;
-  return {q.codes_t, q.scales_t, mx_pitch(rows, q.format), mx_tiles(rows)};
+int codes_side(fp4_ctx* ctx, Side* s, const uint8_t* codes, int64_t rows, int64_t cols, int format) {
+  const int64_t pitch = mx_pitch(cols, format);
+  const int row = code_row_bytes(format);
+  s->wide = true;
+  return make_map(ctx, &s->map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, rows, pitch, row, row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+int codes_along(fp4_ctx* ctx, Codes* c, const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
+  c->on = q.codes != nullptr;
+  c->scales = q.scales;
+  c->tiles = mx_tiles(cols);
+  return c->on ? codes_side(ctx, &c->codes, q.codes, rows, cols, q.format) : FP4_OK;
+}
+int codes_across(fp4_ctx* ctx, Codes* c, const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
+  c->on = q.codes_t != nullptr;
+  c->scales = q.scales_t;
+  c->tiles = mx_tiles(rows);
+  return c->on ? codes_side(ctx, &c->codes, q.codes_t, cols, rows, q.format) : FP4_OK;
 }
 template <auto KERNEL, class A>
-int launch_tiles(int device, int64_t rows, int64_t cols, size_t smem, cudaStream_t stream, const A& args) {
-  const int64_t n = mx_tiles(rows) * mx_tiles(cols);
-  if (n > 0x7FFFFFFF) return FP4_ERR_SHAPE;
-  if (smem > 40 * 1024)
-    FP4_CUDA_TRY(mx_allow_smem<KERNEL>(device, int(smem)));
-  KERNEL<<<unsigned(n), THREADS, smem, stream>>>(args);
-  FP4_CUDA_TRY(cudaGetLastError());
-  return FP4_OK;
+int launch_tiles(fp4_ctx* ctx, int64_t rows, int64_t cols, int most_smem, int smem, cudaStream_t stream, const A& args) {
+  FP4_CUDA_TRY(mx_allow_smem<KERNEL>(ctx->device, 1024 + most_smem));
+  return mx_launch<KERNEL>(dim3(unsigned(mx_tiles(rows) * mx_tiles(cols))), THREADS, 1024 + smem, 1, stream, args);
 }
 
 template <class T, int FMT>
-int quantize_as(int device, cudaStream_t stream, const QuantArgs& a) {
-  const size_t smem = MX_TILE * MX_TILE * sizeof(T);
-  if (a.along.codes && a.across.codes) return launch_tiles<mx_quantize_kernel<T, FMT, true, true>>(device, a.rows, a.cols, smem, stream, a);
-  if (a.across.codes) return launch_tiles<mx_quantize_kernel<T, FMT, false, true>>(device, a.rows, a.cols, smem, stream, a);
-  return launch_tiles<mx_quantize_kernel<T, FMT, true, false>>(device, a.rows, a.cols, 0, stream, a);
+int quantize_as(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a) {
+  constexpr int codes = MX_TILE * code_row_bytes(FMT), one = tile_bytes<T>() + codes;
+  if (a.along.on && a.across.on) return launch_tiles<mx_quantize_kernel<T, FMT, true, true>>(ctx, a.rows, a.cols, one + codes, one + codes, stream, a);
+  if (a.across.on) return launch_tiles<mx_quantize_kernel<T, FMT, false, true>>(ctx, a.rows, a.cols, one, one, stream, a);
+  return launch_tiles<mx_quantize_kernel<T, FMT, true, false>>(ctx, a.rows, a.cols, one, one, stream, a);
 }
 template <class T>
 int quantize_from(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a, const fp4_mx_tensor& q) {
   if (q.format == FP4_MX_NVFP4 && !(q.flags & FP4_MX_AMAX_GIVEN)) {
     FP4_CUDA_TRY(cudaMemsetAsync(q.amax, 0, sizeof(float), stream));
-    const int64_t n = (a.rows * ((a.cols + 7) / 8) + 4 * THREADS - 1) / (4 * THREADS), most = int64_t(ctx->num_sms) * 8;
+    const AmaxArgs m = {a.x.p, a.rows, a.cols, a.x.ld, a.x.wide, reinterpret_cast<uint32_t*>(q.amax)};
+    const int64_t piece = a.x.wide ? 256 * 16 / int(sizeof(T)) : 256, n = (a.rows * ((a.cols + piece - 1) / piece) + 7) / 8, most = int64_t(ctx->num_sms) * 4;
     KernelScope scope(ctx, stream, KC_ABSMAX, 1);
-    mx_amax_kernel<T><<<unsigned(n < most ? n : most), THREADS, 0, stream>>>(a.x, a.rows, a.cols, a.ld, a.wide, reinterpret_cast<uint32_t*>(q.amax));
-    FP4_CUDA_TRY(cudaGetLastError());
+    const int rc = mx_launch<mx_amax_kernel<T>>(dim3(unsigned(n < most ? n : most)), THREADS, 0, 1, stream, m);
+    if (rc != FP4_OK) return rc;
   }
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (q.format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(ctx->device, stream, a);
-  if (q.format == FP4_MX_NVFP4) return quantize_as<T, FP4_MX_NVFP4>(ctx->device, stream, a);
-  return quantize_as<T, FP4_MX_E4M3>(ctx->device, stream, a);
+  if (q.format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(ctx, stream, a);
+  if (q.format == FP4_MX_NVFP4) return quantize_as<T, FP4_MX_NVFP4>(ctx, stream, a);
+  return quantize_as<T, FP4_MX_E4M3>(ctx, stream, a);
+}
+
+template <class T, int FMT>
+int dequantize_as(fp4_ctx* ctx, cudaStream_t stream, const DequantArgs& a) {
+  constexpr int smem = tile_bytes<T>() + MX_TILE * code_row_bytes(FMT);
+  return launch_tiles<mx_dequantize_kernel<T, FMT>>(ctx, a.rows, a.cols, smem, smem, stream, a);
+}
+template <class T>
+int dequantize_to(fp4_ctx* ctx, cudaStream_t stream, const DequantArgs& a, int format) {
+  if (format == FP4_MX_E2M1) return dequantize_as<T, FP4_MX_E2M1>(ctx, stream, a);
+  if (format == FP4_MX_NVFP4) return dequantize_as<T, FP4_MX_NVFP4>(ctx, stream, a);
+  return dequantize_as<T, FP4_MX_E4M3>(ctx, stream, a);
 }
 
 template <class T>
-int dequantize_to(int device, cudaStream_t stream, const DequantArgs& a, int format) {
-  if (format == FP4_MX_E2M1) return launch_tiles<mx_dequantize_kernel<T, FP4_MX_E2M1>>(device, a.rows, a.cols, 0, stream, a);
-  if (format == FP4_MX_NVFP4) return launch_tiles<mx_dequantize_kernel<T, FP4_MX_NVFP4>>(device, a.rows, a.cols, 0, stream, a);
-  return launch_tiles<mx_dequantize_kernel<T, FP4_MX_E4M3>>(device, a.rows, a.cols, 0, stream, a);
+int swiglu_as(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, bool bwd) {
+  const int codes4 = MX_TILE * 64, codes8 = MX_TILE * 128;
+  const int more = (a.along.on ? codes4 : 0) + (a.across.on ? codes4 : 0), tiles = 2 * tile_bytes<T>();
+  const int most = tiles + 2 * codes8 + 2 * codes4;
+  if (bwd) {
+    const int smem = tiles + 2 * codes8 + more;
+    if (a.has_h || more) return launch_tiles<mx_swiglu_bwd_kernel<T, true>>(ctx, a.rows, a.cols, most, smem, stream, a);
+    return launch_tiles<mx_swiglu_bwd_kernel<T, false>>(ctx, a.rows, a.cols, most, smem, stream, a);
+  }
+  if (a.ckpt_gate.on) return launch_tiles<mx_swiglu_fwd_kernel<T, true>>(ctx, a.rows, a.cols, most, tiles + 2 * codes8 + more, stream, a);
+  return launch_tiles<mx_swiglu_fwd_kernel<T, false>>(ctx, a.rows, a.cols, most, tiles + more, stream, a);
 }
-
-template <class T>
-int swiglu_as(int device, cudaStream_t stream, const SwigluArgs& a, bool bwd, bool keep) {
-  const size_t smem = a.across.codes ? MX_TILE * MX_TILE * sizeof(T) : 0;
-  if (bwd)
-    return smem ? launch_tiles<mx_swiglu_kernel<T, true, false, true>>(device, a.rows, a.cols, smem, stream, a)
-                : launch_tiles<mx_swiglu_kernel<T, true, false, false>>(device, a.rows, a.cols, 0, stream, a);
-  if (keep)
-    return smem ? launch_tiles<mx_swiglu_kernel<T, false, true, true>>(device, a.rows, a.cols, smem, stream, a)
-                : launch_tiles<mx_swiglu_kernel<T, false, true, false>>(device, a.rows, a.cols, 0, stream, a);
-  return smem ? launch_tiles<mx_swiglu_kernel<T, false, false, true>>(device, a.rows, a.cols, smem, stream, a)
-              : launch_tiles<mx_swiglu_kernel<T, false, false, false>>(device, a.rows, a.cols, 0, stream, a);
-}
-int swiglu(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, int dtype, bool bwd, bool keep) {
+int swiglu(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, int dtype, bool bwd) {
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (dtype == FP4_DTYPE_BF16) return swiglu_as<__nv_bfloat16>(ctx->device, stream, a, bwd, keep);
-  if (dtype == FP4_DTYPE_FP16) return swiglu_as<__half>(ctx->device, stream, a, bwd, keep);
-  return swiglu_as<float>(ctx->device, stream, a, bwd, keep);
+  if (dtype == FP4_DTYPE_BF16) return swiglu_as<__nv_bfloat16>(ctx, stream, a, bwd);
+  if (dtype == FP4_DTYPE_FP16) return swiglu_as<__half>(ctx, stream, a, bwd);
+  return swiglu_as<float>(ctx, stream, a, bwd);
 }
 
 }  // namespace
 
 int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, MxMatrix x, int dtype, const fp4_mx_tensor& q, int32_t* status) {
   QuantArgs a = {};
-  a.x = x.p;
   a.rows = q.rows;
   a.cols = q.cols;
-  a.ld = x.ld;
-  a.wide = rows_aligned(x.p, x.ld, dtype);
-  a.along = codes_along(q, q.rows, q.cols);
-  a.across = codes_across(q, q.rows, q.cols);
   a.amax = reinterpret_cast<const uint32_t*>(q.amax);
   a.status = status;
+  int rc = matrix_side(ctx, &a.x, x, q.rows, q.cols, dtype, false);
+  if (rc == FP4_OK) rc = codes_along(ctx, &a.along, q, q.rows, q.cols);
+  if (rc == FP4_OK) rc = codes_across(ctx, &a.across, q, q.rows, q.cols);
+  if (rc != FP4_OK) return rc;
   if (dtype == FP4_DTYPE_BF16) return quantize_from<__nv_bfloat16>(ctx, stream, a, q);
   if (dtype == FP4_DTYPE_FP16) return quantize_from<__half>(ctx, stream, a, q);
   return quantize_from<float>(ctx, stream, a, q);
 }
 
 int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes, const uint8_t* scales, const float* amax,
-                         int64_t rows, int64_t cols, int format, void* out, int64_t ld, int dtype) {
-  const DequantArgs a = {codes, scales, reinterpret_cast<const uint32_t*>(amax), rows, cols, out, ld, rows_aligned(out, ld, dtype)};
+                         int64_t rows, int64_t cols, int format, MxMatrix out, int dtype, int32_t* status) {
+  DequantArgs a = {};
+  a.scales = scales;
+  a.amax = reinterpret_cast<const uint32_t*>(amax);
+  a.rows = rows;
+  a.cols = cols;
+  a.status = status;
+  int rc = codes_side(ctx, &a.codes, codes, rows, cols, format);
+  if (rc == FP4_OK) rc = matrix_side(ctx, &a.out, out, rows, cols, dtype, true);
+  if (rc != FP4_OK) return rc;
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (dtype == FP4_DTYPE_BF16) return dequantize_to<__nv_bfloat16>(ctx->device, stream, a, format);
-  if (dtype == FP4_DTYPE_FP16) return dequantize_to<__half>(ctx->device, stream, a, format);
-  return dequantize_to<float>(ctx->device, stream, a, format);
+  if (dtype == FP4_DTYPE_BF16) return dequantize_to<__nv_bfloat16>(ctx, stream, a, format);
+  if (dtype == FP4_DTYPE_FP16) return dequantize_to<__half>(ctx, stream, a, format);
+  return dequantize_to<float>(ctx, stream, a, format);
 }
 
 int launch_mx_swiglu_fwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix gate, MxMatrix up, int64_t rows, int64_t cols, int dtype,
                          MxMatrix h, const fp4_mx_tensor* ckpt_gate, const fp4_mx_tensor* ckpt_up, const fp4_mx_tensor* q,
                          int32_t* status) {
   SwigluArgs a = {};
-  a.gate = gate.p;
-  a.up = up.p;
-  a.ld_gate = gate.ld;
-  a.ld_up = up.ld;
-  if (ckpt_gate) {
-    a.ckpt_gate = codes_along(*ckpt_gate, rows, cols);
-    a.ckpt_up = codes_along(*ckpt_up, rows, cols);
-  }
-  a.h = const_cast<void*>(h.p);
-  a.ld_h = h.ld;
-  if (q) {
-    a.along = codes_along(*q, rows, cols);
-    a.across = codes_across(*q, rows, cols);
-  }
   a.rows = rows;
   a.cols = cols;
-  a.wide = rows_aligned(gate.p, gate.ld, dtype) && rows_aligned(up.p, up.ld, dtype) && (!h.p || rows_aligned(h.p, h.ld, dtype));
   a.status = status;
-  return swiglu(ctx, stream, a, dtype, false, ckpt_gate != nullptr);
+  a.has_h = h.p != nullptr;
+  int rc = matrix_side(ctx, &a.gate, gate, rows, cols, dtype, false);
+  if (rc == FP4_OK) rc = matrix_side(ctx, &a.up, up, rows, cols, dtype, false);
+  if (rc == FP4_OK && a.has_h) rc = matrix_side(ctx, &a.h, h, rows, cols, dtype, true);
+  if (rc == FP4_OK && ckpt_gate) rc = codes_along(ctx, &a.ckpt_gate, *ckpt_gate, rows, cols);
+  if (rc == FP4_OK && ckpt_up) rc = codes_along(ctx, &a.ckpt_up, *ckpt_up, rows, cols);
+  if (rc == FP4_OK && q) rc = codes_along(ctx, &a.along, *q, rows, cols);
+  if (rc == FP4_OK && q) rc = codes_across(ctx, &a.across, *q, rows, cols);
+  return rc != FP4_OK ? rc : swiglu(ctx, stream, a, dtype, false);
 }
 
 int launch_mx_swiglu_bwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix dh, const fp4_mx_tensor& gate, const fp4_mx_tensor& up,
                          int64_t rows, int64_t cols, int dtype, MxMatrix dgate, MxMatrix dup, MxMatrix h,
                          const fp4_mx_tensor* q, int32_t* status) {
   SwigluArgs a = {};
-  a.dh = dh.p;
-  a.ld_dh = dh.ld;
-  a.ckpt_gate = codes_along(gate, rows, cols);
-  a.ckpt_up = codes_along(up, rows, cols);
-  a.dgate = const_cast<void*>(dgate.p);
-  a.dup = const_cast<void*>(dup.p);
-  a.ld_dgate = dgate.ld;
-  a.ld_dup = dup.ld;
-  a.h = const_cast<void*>(h.p);
-  a.ld_h = h.ld;
-  if (q) {
-    a.along = codes_along(*q, rows, cols);
-    a.across = codes_across(*q, rows, cols);
-  }
   a.rows = rows;
   a.cols = cols;
-  a.wide = rows_aligned(dh.p, dh.ld, dtype) && rows_aligned(dgate.p, dgate.ld, dtype) && rows_aligned(dup.p, dup.ld, dtype) &&
-           (!h.p || rows_aligned(h.p, h.ld, dtype));
   a.status = status;
-  return swiglu(ctx, stream, a, dtype, true, false);
+  a.has_h = h.p != nullptr;
+  int rc = matrix_side(ctx, &a.dh, dh, rows, cols, dtype, false);
+  if (rc == FP4_OK) rc = matrix_side(ctx, &a.gate, dgate, rows, cols, dtype, true);
+  if (rc == FP4_OK) rc = matrix_side(ctx, &a.up, dup, rows, cols, dtype, true);
+  if (rc == FP4_OK && a.has_h) rc = matrix_side(ctx, &a.h, h, rows, cols, dtype, true);
+  if (rc == FP4_OK) rc = codes_along(ctx, &a.ckpt_gate, gate, rows, cols);
+  if (rc == FP4_OK) rc = codes_along(ctx, &a.ckpt_up, up, rows, cols);
+  if (rc == FP4_OK && q) rc = codes_along(ctx, &a.along, *q, rows, cols);
+  if (rc == FP4_OK && q) rc = codes_across(ctx, &a.across, *q, rows, cols);
+  return rc != FP4_OK ? rc : swiglu(ctx, stream, a, dtype, true);
 }

@@ -46,7 +46,7 @@ def declare(lib: C.CDLL):
     lib.fp4_mx_pitch.argtypes, lib.fp4_mx_pitch.restype = [i64, i32], i64
     lib.fp4_mx_scale_bytes.argtypes, lib.fp4_mx_scale_bytes.restype = [i64, i64, i32], i64
     lib.fp4_mx_workspace_bytes.argtypes, lib.fp4_mx_workspace_bytes.restype = [i64, i64, i64], C.c_size_t
-    for name, args in (("quantize", [mat, ten, vp]), ("dequantize", [ten, i32, mat]), ("gemm", [ten, ten, i32, mat, vp]),
+    for name, args in (("quantize", [mat, ten, vp]), ("dequantize", [ten, i32, mat, vp]), ("gemm", [ten, ten, i32, mat, vp]),
                        ("linear_fwd", [mat, mat, i64, i64, i64, i32, mat, ten, ten, vp]),
                        ("linear_bwd", [mat, ten, ten, i64, i64, i64, i32, mat, mat, vp]),
                        ("swiglu_fwd", [mat, mat, i64, i64, mat, ten, ten, ten, vp]),
@@ -125,7 +125,8 @@ def fp4_mx_dequantize(ctx: Context, q: MXTensor, transposed: bool = False, dtype
     if out is None:
         out = _new(ctx, *shape, dtype)
     assert out.shape == shape
-    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream_of(ctx.device), q.ref, int(transposed), _matrix(ctx, out)))
+    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream_of(ctx.device), q.ref, int(transposed), _matrix(ctx, out),
+                                     ctx.status.data_ptr()))
     return out
 
 

@@ -85,9 +85,9 @@ def test_quantize_refusals(lib, ctx):
 
 @no_gpu
 def test_dequantize_refusals(lib, ctx):
-    call = lambda q, t, o, c=ctx: lib.fp4_mx_dequantize(c, None, ref(q), t, ref(o))            # noqa: E731
+    call = lambda q, t, o, c=ctx, st=P: lib.fp4_mx_dequantize(c, None, ref(q), t, ref(o), st)   # noqa: E731
     assert passes(call(ten(), 0, mat())) and passes(call(ten(), 1, mat(ld=8)))
-    assert call(ten(), 0, None) == NULL and call(None, 0, mat()) == NULL and call(ten(), 0, mat(), c=None) == NULL
+    assert call(ten(), 0, None) == NULL and call(None, 0, mat()) == NULL and call(ten(), 0, mat(), c=None) == NULL and call(ten(), 0, mat(), st=None) == NULL
     assert call(ten(codes_t=False), 1, mat()) == NULL and call(ten(codes=False), 0, mat()) == NULL
     assert call(ten(), 1, mat(ld=7)) == RANGE and call(ten(), 0, mat(ld=63)) == RANGE
     assert call(ten(), 0, mat(data=None)) == NULL and call(ten(rows=0), 0, mat(data=None)) == 0
