@@ -226,6 +226,13 @@ __device__ __forceinline__ Run<T> load_run(const uint8_t* tile, int row, int run
   }
   return v;
 }
+// What comes behind starts from these registers: the compiler does not spread several steps' values over more registers than three blocks
+// an SM leave a thread (80).
+template <class T>
+__device__ __forceinline__ void in_order(Run<T>& v) {
+#pragma unroll
+  for (int i = 0; i < Run<T>::WORDS; ++i) asm volatile("" : "+r"(v.w[i]));
+}
 // The 32 E4M3 codes of a run.
 struct Run8 {
   uint32_t w[8];
@@ -264,6 +271,17 @@ __device__ __forceinline__ void encode_run(int r, int run, float inv_tensor, Pai
   } else {
     *reinterpret_cast<uint4*>(s_codes + at64(r, run * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
   }
+}
+// E4M3 codes of a run into staged codes of 64 columns (two runs), 64-byte rows.
+template <class T>
+__device__ __forceinline__ void keep_run(const Run<T>& v, int r, int run, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+  const Scale s = scale_of<T, FP4_MX_E4M3>(v.amax(0, 32), 1.0f);
+  bad |= !s.finite;
+  s_scale[scale_at(r, run)] = uint8_t(s.byte);
+  uint32_t w[8];
+  encode_block<FP4_MX_E4M3, 32>(s, [&](int i) { return v.pair(i); }, w);
+  *reinterpret_cast<uint4*>(s_codes + at64(r, (run & 1) * 32)) = make_uint4(w[0], w[1], w[2], w[3]);
+  *reinterpret_cast<uint4*>(s_codes + at64(r, (run & 1) * 32 + 16)) = make_uint4(w[4], w[5], w[6], w[7]);
 }
 // Blocks along the rows: the thread's run.
 template <class T, int FMT>
@@ -651,16 +669,17 @@ __device__ __forceinline__ void finish_h(const SwigluArgs& a, const TileAt& at, 
   if (a.along.on) copy_scales(a.along.scales + (at.row * a.along.tiles + at.col) * 512, s_scale[0], 512);
   if (a.across.on) copy_scales(a.across.scales + (at.col * a.across.tiles + at.row) * 512, s_scale[1], 512);
 }
-// Shared memory: gate (then h), up, and as they are wanted the checkpoints' codes and h's in either direction.
+// Shared memory: gate (then h), up (then the checkpoints' codes, in four pieces of 128 rows x 64 bytes: gate and up of either half of the
+// columns), and h's codes in either direction as they are wanted.  64 KB of 16-bit inputs: three blocks an SM.  A thread takes its part of up
+// into registers before anyone writes codes there.  (Codes beside the inputs, two blocks an SM: 16384 x 13824 358 us; codes from the
+// threads to global memory, 16 bytes a row of each: 434.)
 template <class T, bool KEEP>
-__global__ void __launch_bounds__(THREADS) mx_swiglu_fwd_kernel(const __grid_constant__ SwigluArgs a) {
-  constexpr int CODES8 = MX_TILE * 128, CODES4 = MX_TILE * 64;
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd_kernel(const __grid_constant__ SwigluArgs a) {
+  constexpr int CODES4 = MX_TILE * 64, PIECE = MX_TILE * 64;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* t_up = tile + tile_bytes<T>();
-  uint8_t* s_gate = t_up + tile_bytes<T>();
-  uint8_t* s_up = s_gate + (KEEP ? CODES8 : 0);
-  uint8_t* s_along = s_up + (KEEP ? CODES8 : 0);
+  uint8_t* s_along = t_up + tile_bytes<T>();
   uint8_t* s_across = s_along + (a.along.on ? CODES4 : 0);
   __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
   __shared__ Loader l;
@@ -683,19 +702,26 @@ __global__ void __launch_bounds__(THREADS) mx_swiglu_fwd_kernel(const __grid_con
   __syncthreads();
   if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
   bool bad = false;
-  const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
-#pragma unroll 1
-  for (int run = run0; run < run0 + 2; ++run) {
+  const int r = threadIdx.x & 127, half = threadIdx.x >> 7;
+  Run<T> u[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) u[i] = load_run<T>(t_up, r, 2 * half + i);
+  if (KEEP) __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int run = 2 * half + i;
     Run<T> g = load_run<T>(tile, r, run);
-    const Run<T> u = load_run<T>(t_up, r, run);
     if (KEEP) {
-      encode_along<T, FP4_MX_E4M3>(g, r, run, 1.0f, s_gate, s_scale[2], bad);
-      encode_along<T, FP4_MX_E4M3>(u, r, run, 1.0f, s_up, s_scale[3], bad);
+      keep_run(g, r, run, t_up + half * PIECE, s_scale[2], bad);
+      in_order(g);
+      keep_run(u[i], r, run, t_up + (2 + half) * PIECE, s_scale[3], bad);
+      in_order(u[i]);
+      in_order(g);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float g0 = g.get(2 * i), g1 = g.get(2 * i + 1);
-      g.set_pair(i, g0 * sigmoid(g0).s * u.get(2 * i), g1 * sigmoid(g1).s * u.get(2 * i + 1));
+    for (int k = 0; k < 16; ++k) {
+      const float g0 = g.get(2 * k), g1 = g.get(2 * k + 1);
+      g.set_pair(k, g0 * sigmoid(g0).s * u[i].get(2 * k), g1 * sigmoid(g1).s * u[i].get(2 * k + 1));
     }
     if (a.has_h || a.across.on) store_run(tile, r, run, g);
     if (a.along.on) encode_along<T, FP4_MX_E2M1>(g, r, run, 1.0f, s_along, s_scale[0], bad);
@@ -703,27 +729,28 @@ __global__ void __launch_bounds__(THREADS) mx_swiglu_fwd_kernel(const __grid_con
   if (a.across.on) __syncthreads();
   finish_h<T>(a, at, tile, s_along, s_across, s_scale, bad);
   if (KEEP) {
-    if (threadIdx.x == 0) {
-      tma_store_2d(&a.ckpt_gate.codes.map, s_gate, int(at.col) * 128, int(row0));
-      tma_store_2d(&a.ckpt_up.codes.map, s_up, int(at.col) * 128, int(row0));
-    }
+    if (threadIdx.x == 0)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        tma_store_2d(&a.ckpt_gate.codes.map, t_up + i * PIECE, int(at.col) * 128 + 64 * i, int(row0));
+        tma_store_2d(&a.ckpt_up.codes.map, t_up + (2 + i) * PIECE, int(at.col) * 128 + 64 * i, int(row0));
+      }
     copy_scales(a.ckpt_gate.scales + (at.row * a.ckpt_gate.tiles + at.col) * 512, s_scale[2], 512);
     copy_scales(a.ckpt_up.scales + (at.row * a.ckpt_up.tiles + at.col) * 512, s_scale[3], 512);
   }
   report(bad, a.status);
   if (threadIdx.x == 0) tma_store_wait_all();
 }
-// Shared memory: dh (then d_gate), d_up (then h), the checkpoints' codes, and h's as they are wanted.  h is made behind the gradients, once
-// their copies have read the tile that it takes: a tile of its own would leave one block an SM.
+// Shared memory: dh (then d_gate), the checkpoints' codes (then d_up), and as they are wanted h and its codes.  A thread takes its codes into
+// registers before anyone writes d_up there.
 template <class T, bool H>
-__global__ void __launch_bounds__(THREADS) mx_swiglu_bwd_kernel(const __grid_constant__ SwigluArgs a) {
+__global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_swiglu_bwd_kernel(const __grid_constant__ SwigluArgs a) {
   constexpr int CODES8 = MX_TILE * 128, CODES4 = MX_TILE * 64;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* t_up = tile + tile_bytes<T>();
-  uint8_t* s_gate = t_up + tile_bytes<T>();
-  uint8_t* s_up = s_gate + CODES8;
-  uint8_t* s_along = s_up + CODES8;
+  uint8_t* t_h = t_up + tile_bytes<T>();
+  uint8_t* s_along = t_h + (H ? tile_bytes<T>() : 0);
   uint8_t* s_across = s_along + (H && a.along.on ? CODES4 : 0);
   __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
   __shared__ Loader l;
@@ -738,8 +765,8 @@ __global__ void __launch_bounds__(THREADS) mx_swiglu_bwd_kernel(const __grid_con
   mx_let_next_start();
   if (threadIdx.x == 0) {
     mbar_arrive_expect_tx(&l.bar, 2 * CODES8 + (a.dh.wide ? tile_bytes<T>() : 0));
-    tma_load_2d(s_gate, &a.ckpt_gate.codes.map, &l.bar, int(at.col) * 128, int(row0));
-    tma_load_2d(s_up, &a.ckpt_up.codes.map, &l.bar, int(at.col) * 128, int(row0));
+    tma_load_2d(t_up, &a.ckpt_gate.codes.map, &l.bar, int(at.col) * 128, int(row0));
+    tma_load_2d(t_up + CODES8, &a.ckpt_up.codes.map, &l.bar, int(at.col) * 128, int(row0));
     if (a.dh.wide) request_tile<T>(a.dh, &l, tile, row0, col0);
   }
   if (!a.dh.wide) copy_tile_in<T>(a.dh, tile, row0, col0, a.rows, a.cols);
@@ -747,32 +774,46 @@ __global__ void __launch_bounds__(THREADS) mx_swiglu_bwd_kernel(const __grid_con
   copy_scales(s_scale[3], a.ckpt_up.scales + (at.row * a.ckpt_up.tiles + at.col) * 512, 512);
   __syncthreads();
   if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
-  const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
-#pragma unroll 1
-  for (int run = run0; run < run0 + 2; ++run) {
-    const float sg = scale_value<FP4_MX_E4M3>(s_scale[2][scale_at(r, run)]), su = scale_value<FP4_MX_E4M3>(s_scale[3][scale_at(r, run)]);
-    const Run8 cg = load_run8(s_gate, r, run), cu = load_run8(s_up, r, run);
-    Run<T> d = load_run<T>(tile, r, run), e;
+  bool bad = false;
+  const int r = threadIdx.x & 127, half = threadIdx.x >> 7;
+  Run8 cg[2], cu[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float g[4], u[4], dg[4], du[4];
-      decode4_e4m3(cg.w[i], sg, g);
-      decode4_e4m3(cu.w[i], su, u);
+  for (int i = 0; i < 2; ++i) {
+    cg[i] = load_run8(t_up, r, 2 * half + i);
+    cu[i] = load_run8(t_up + CODES8, r, 2 * half + i);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int run = 2 * half + i;
+    const float sg = scale_value<FP4_MX_E4M3>(s_scale[2][scale_at(r, run)]), su = scale_value<FP4_MX_E4M3>(s_scale[3][scale_at(r, run)]);
+    Run<T> d = load_run<T>(tile, r, run), e, h;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      float g[4], u[4], dg[4], du[4], hv[4];
+      decode4_e4m3(cg[i].w[q], sg, g);
+      decode4_e4m3(cu[i].w[q], su, u);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const Sigmoid s = sigmoid(g[k]);
-        const float gs = g[k] * s.s, dh = d.get(4 * i + k);
+        const float gs = g[k] * s.s, dh = d.get(4 * q + k);
         du[k] = dh * gs;
         dg[k] = dh * u[k] * fmaf(gs, s.rest, s.s);         // d/dg g s = s (1 + g (1 - s)) = s + g s (1 - s)
+        hv[k] = gs * u[k];
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        d.set_pair(2 * i + k, dg[2 * k], dg[2 * k + 1]);
-        e.set_pair(2 * i + k, du[2 * k], du[2 * k + 1]);
+        d.set_pair(2 * q + k, dg[2 * k], dg[2 * k + 1]);
+        e.set_pair(2 * q + k, du[2 * k], du[2 * k + 1]);
+        if (H) h.set_pair(2 * q + k, hv[2 * k], hv[2 * k + 1]);
       }
     }
     store_run(tile, r, run, d);
     store_run(t_up, r, run, e);
+    if (H) {
+      if (a.has_h || a.across.on) store_run(t_h, r, run, h);
+      if (a.along.on) encode_along<T, FP4_MX_E2M1>(h, r, run, 1.0f, s_along, s_scale[0], bad);
+    }
   }
   fence_async_smem();
   __syncthreads();
@@ -783,28 +824,7 @@ __global__ void __launch_bounds__(THREADS) mx_swiglu_bwd_kernel(const __grid_con
   if (!a.up.wide) copy_tile_out<T>(a.up, t_up, row0, col0, a.rows, a.cols);
   if (!a.gate.wide) copy_tile_out<T>(a.gate, tile, row0, col0, a.rows, a.cols);
   if (H) {
-    if (threadIdx.x == 0) tma_store_wait_read_0();
-    __syncthreads();
-    bool bad = false;
-#pragma unroll 1
-    for (int run = run0; run < run0 + 2; ++run) {
-      const float sg = scale_value<FP4_MX_E4M3>(s_scale[2][scale_at(r, run)]), su = scale_value<FP4_MX_E4M3>(s_scale[3][scale_at(r, run)]);
-      const Run8 cg = load_run8(s_gate, r, run), cu = load_run8(s_up, r, run);
-      Run<T> v;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float g[4], u[4];
-        decode4_e4m3(cg.w[i], sg, g);
-      decode4_e4m3(cu.w[i], su, u);
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          v.set_pair(2 * i + k, g[2 * k] * sigmoid(g[2 * k]).s * u[2 * k], g[2 * k + 1] * sigmoid(g[2 * k + 1]).s * u[2 * k + 1]);
-      }
-      store_run(t_up, r, run, v);
-      if (a.along.on) encode_along<T, FP4_MX_E2M1>(v, r, run, 1.0f, s_along, s_scale[0], bad);
-    }
-    if (a.across.on) __syncthreads();
-    finish_h<T>(a, at, t_up, s_along, s_across, s_scale, bad);
+    finish_h<T>(a, at, t_h, s_along, s_across, s_scale, bad);
     report(bad, a.status);
   }
   if (threadIdx.x == 0) tma_store_wait_all();
@@ -838,17 +858,17 @@ int matrix_side(fp4_ctx* ctx, Side* s, MxMatrix m, int64_t rows, int64_t cols, i
                                                              : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   return make_map(ctx, &s->map, type, m.p, cols, rows, m.ld * elt, 128 / elt, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-int codes_side(fp4_ctx* ctx, Side* s, const uint8_t* codes, int64_t rows, int64_t cols, int format) {
+int codes_side(fp4_ctx* ctx, Side* s, const uint8_t* codes, int64_t rows, int64_t cols, int format, int row = 0) {
   const int64_t pitch = mx_pitch(cols, format);
-  const int row = code_row_bytes(format);
+  if (!row) row = code_row_bytes(format);
   s->wide = true;
   return make_map(ctx, &s->map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, pitch, rows, pitch, row, row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
-int codes_along(fp4_ctx* ctx, Codes* c, const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
+int codes_along(fp4_ctx* ctx, Codes* c, const fp4_mx_tensor& q, int64_t rows, int64_t cols, int box_bytes = 0) {
   c->on = q.codes != nullptr;
   c->scales = q.scales;
   c->tiles = mx_tiles(cols);
-  return c->on ? codes_side(ctx, &c->codes, q.codes, rows, cols, q.format) : FP4_OK;
+  return c->on ? codes_side(ctx, &c->codes, q.codes, rows, cols, q.format, box_bytes) : FP4_OK;
 }
 int codes_across(fp4_ctx* ctx, Codes* c, const fp4_mx_tensor& q, int64_t rows, int64_t cols) {
   c->on = q.codes_t != nullptr;
@@ -899,16 +919,13 @@ int dequantize_to(fp4_ctx* ctx, cudaStream_t stream, const DequantArgs& a, int f
 
 template <class T>
 int swiglu_as(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, bool bwd) {
-  const int codes4 = MX_TILE * 64, codes8 = MX_TILE * 128;
-  const int more = (a.along.on ? codes4 : 0) + (a.across.on ? codes4 : 0), tiles = 2 * tile_bytes<T>();
-  const int most = tiles + 2 * codes8 + 2 * codes4;
-  if (bwd) {
-    const int smem = tiles + 2 * codes8 + more;
-    if (a.has_h || more) return launch_tiles<mx_swiglu_bwd_kernel<T, true>>(ctx, a.rows, a.cols, most, smem, stream, a);
-    return launch_tiles<mx_swiglu_bwd_kernel<T, false>>(ctx, a.rows, a.cols, most, smem, stream, a);
-  }
-  if (a.ckpt_gate.on) return launch_tiles<mx_swiglu_fwd_kernel<T, true>>(ctx, a.rows, a.cols, most, tiles + 2 * codes8 + more, stream, a);
-  return launch_tiles<mx_swiglu_fwd_kernel<T, false>>(ctx, a.rows, a.cols, most, tiles + more, stream, a);
+  constexpr int codes4 = MX_TILE * 64, tile = tile_bytes<T>();
+  const int more = (a.along.on ? codes4 : 0) + (a.across.on ? codes4 : 0);
+  if (bwd && (a.has_h || more))
+    return launch_tiles<mx_swiglu_bwd_kernel<T, true>>(ctx, a.rows, a.cols, 3 * tile + 2 * codes4, 3 * tile + more, stream, a);
+  if (bwd) return launch_tiles<mx_swiglu_bwd_kernel<T, false>>(ctx, a.rows, a.cols, 2 * tile, 2 * tile, stream, a);
+  if (a.ckpt_gate.on) return launch_tiles<mx_swiglu_fwd_kernel<T, true>>(ctx, a.rows, a.cols, 2 * tile + 2 * codes4, 2 * tile + more, stream, a);
+  return launch_tiles<mx_swiglu_fwd_kernel<T, false>>(ctx, a.rows, a.cols, 2 * tile + 2 * codes4, 2 * tile + more, stream, a);
 }
 int swiglu(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, int dtype, bool bwd) {
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
@@ -962,8 +979,8 @@ int launch_mx_swiglu_fwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix gate, MxMat
   int rc = matrix_side(ctx, &a.gate, gate, rows, cols, dtype, false);
   if (rc == FP4_OK) rc = matrix_side(ctx, &a.up, up, rows, cols, dtype, false);
   if (rc == FP4_OK && a.has_h) rc = matrix_side(ctx, &a.h, h, rows, cols, dtype, true);
-  if (rc == FP4_OK && ckpt_gate) rc = codes_along(ctx, &a.ckpt_gate, *ckpt_gate, rows, cols);
-  if (rc == FP4_OK && ckpt_up) rc = codes_along(ctx, &a.ckpt_up, *ckpt_up, rows, cols);
+  if (rc == FP4_OK && ckpt_gate) rc = codes_along(ctx, &a.ckpt_gate, *ckpt_gate, rows, cols, 64);
+  if (rc == FP4_OK && ckpt_up) rc = codes_along(ctx, &a.ckpt_up, *ckpt_up, rows, cols, 64);
   if (rc == FP4_OK && q) rc = codes_along(ctx, &a.along, *q, rows, cols);
   if (rc == FP4_OK && q) rc = codes_across(ctx, &a.across, *q, rows, cols);
   return rc != FP4_OK ? rc : swiglu(ctx, stream, a, dtype, false);
