@@ -23,7 +23,8 @@ E4M3 = np.array([(c & 7) * 2.0 ** -9 if c < 8 else (1 + (c & 7) / 8) * 2.0 ** ((
 
 
 def rn32(v: np.ndarray) -> np.ndarray:
-    return v.astype(np.float32).astype(np.float64)
+    with np.errstate(over="ignore"):                     # (beyond its range: infinity)
+        return v.astype(np.float32).astype(np.float64)
 
 
 def nearest_code(a: np.ndarray, grid: np.ndarray) -> np.ndarray:

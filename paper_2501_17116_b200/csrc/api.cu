@@ -136,6 +136,7 @@ int fp4_create(fp4_ctx** out, int device, size_t workspace_bytes) {
   ctx->workspace_bytes = 0;
   ctx->encode_tiled = nullptr;
   ctx->occ_hist = nullptr;
+  ctx->mx_scratch = nullptr;
   ctx->profile = 0;
   ctx->debug_wait_limit_ns = 0;
   ctx->debug_skip_fill = -1;
@@ -181,6 +182,8 @@ int fp4_create(fp4_ctx** out, int device, size_t workspace_bytes) {
   // counters of the quantile selection (quantisation with clamping): cleared here, once
   ok = ok && cudaMalloc(reinterpret_cast<void**>(&ctx->occ_hist), quantize_persistent_bytes()) == cudaSuccess;
   ok = ok && cudaMemset(ctx->occ_hist, 0, quantize_persistent_bytes()) == cudaSuccess;
+  ok = ok && cudaMalloc(reinterpret_cast<void**>(&ctx->mx_scratch), MX_SCRATCH_WORDS * sizeof(uint32_t)) == cudaSuccess;
+  ok = ok && cudaMemset(ctx->mx_scratch, 0, MX_SCRATCH_WORDS * sizeof(uint32_t)) == cudaSuccess;
   for (auto& s : ctx->side) ok = ok && cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking) == cudaSuccess;
   for (auto& e : ctx->ev) ok = ok && cudaEventCreateWithFlags(&e, cudaEventDisableTiming) == cudaSuccess;
   ok = ok && cudaStreamCreateWithFlags(&ctx->copy_stream, cudaStreamNonBlocking) == cudaSuccess;
@@ -214,6 +217,7 @@ int fp4_destroy(fp4_ctx* ctx) {
   for (auto& e : ctx->host_step_copied)
     if (e) cudaEventDestroy(e);
   if (ctx->workspace) cudaFree(ctx->workspace);
+  if (ctx->mx_scratch) cudaFree(ctx->mx_scratch);
   if (ctx->occ_hist) cudaFree(ctx->occ_hist);      // waits for the GPU, so no graph is running below
   delete ctx->graphs;
   if (ctx->records) {

@@ -34,6 +34,8 @@ struct ProfRecord {
 // of finished outputs for long).
 constexpr int HOST_STEP_SETS = 2;
 
+constexpr int MX_SCRATCH_WORDS = 1024;
+
 class CallGraphs;                     // call_graph.cuh
 
 struct fp4_ctx {
@@ -43,6 +45,7 @@ struct fp4_ctx {
   char*    workspace;
   size_t   workspace_bytes;
   void*    encode_tiled;       // cuTensorMapEncodeTiled, fetched through the runtime
+  uint32_t* mx_scratch;        // block-scaled operands: the blocks' parts of a tensor's amax (MX_SCRATCH_WORDS, the last a ticket)
   uint32_t* occ_hist;          // quantile selection: two sets of global counters, parity, ticket
   cudaStream_t side[2];        // side streams for independent kernel chains inside one call
   cudaEvent_t  ev[10];          // fork / join events of those chains

@@ -29,6 +29,10 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int BOX_BYTES = MX_TILE * 128;                 // 128 rows of 128 bytes
+constexpr int64_t MX_SMALL_BYTES = 64 << 10;             // a tensor up to this size: its amax is found by every block for itself
+// More parts than this are joined by the kernel that finds them: every block of the quantiser reading 592 of them cost 10 us of 16384 x 13824;
+// the join's ticket costs a small tensor 1 us.
+constexpr int MX_FEW_PARTS = 64;
 
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
@@ -146,28 +150,36 @@ __device__ __forceinline__ float e4m3_value(uint32_t byte) {              // fin
 __device__ __forceinline__ float pow2_byte(uint32_t e8) { return __uint_as_float(e8 ? e8 << 23 : 0x400000u); }   // 2^(e8 - 127)
 __device__ __forceinline__ float pow2_int(int k) { return __uint_as_float(uint32_t(k + 127) << 23); }            // -126 <= k <= 127
 
+#define NO_TENSOR_SCALE make_float2(1.0f, 1.0f)
+
 // Scale of a block: its byte, and what its elements are scaled with.
 struct Scale {
   uint32_t byte;
-  float mul;                 // 2^-e; NVFP4: 2^-k
-  float s, inv;              // NVFP4: s and 1 / s rounded
+  float mul;                 // 2^-e; NVFP4: 1 / s rounded, times 2^-k
+  float s;                   // NVFP4: s 2^k
+  bool far;                  // NVFP4: far beyond the given amax
   bool finite;
 };
 template <class T, int FMT>
-__device__ __forceinline__ Scale scale_of(uint32_t amax_pattern, float inv_tensor) {
+__device__ __forceinline__ Scale scale_of(uint32_t amax_pattern, float2 tensor) {
   Scale r;
   r.finite = amax_pattern < TypeOf<T>::INF;                 // patterns of infinities and NaNs lie above all others
   const float amax = TypeOf<T>::value(amax_pattern);
   if constexpr (FMT == FP4_MX_NVFP4) {
     // The quotient by 6, and later those by s, rounded correctly from the correctly rounded reciprocal (Markstein 1990:
     // q + (a - q s) inv in two fused steps); a value that lies on a tie of the format then comes out on it.
-    const float a = amax * inv_tensor, sixth = 1.0f / 6.0f;
+    const float a = fminf(amax * tensor.y, 1e30f), sixth = 1.0f / 6.0f;
     const float q = a * sixth;
     const float v = fmaf(fmaf(-q, 6.0f, a), sixth, q);
     r.byte = e4m3_word(pack2(v, 0.0f), pack2(0.0f, 0.0f)) & 0xFFu;
-    r.s = e4m3_value(r.byte);
-    r.inv = r.byte ? __frcp_rn(r.s) : 0.0f;
-    r.mul = inv_tensor;
+    // 1 / s from the special-function unit's approximation by a Newton step
+    const float s = e4m3_value(r.byte);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    inv = fmaf(inv, fmaf(-s, inv, 1.0f), inv);
+    r.mul = r.byte ? inv * tensor.y : 0.0f;
+    r.s = s * tensor.x;
+    r.far = v > 1e6f;
     if (!r.finite) r.byte = 0x7Fu;
   } else {
     // 6 = 1.5 * 2^2 and 448 = 1.75 * 2^8: the sum carries into the exponent where the mantissa is larger
@@ -181,11 +193,16 @@ __device__ __forceinline__ Scale scale_of(uint32_t amax_pattern, float inv_tenso
 }
 template <int FMT>
 __device__ __forceinline__ f32x2 scaled(f32x2 x, const Scale& s) {
-  const f32x2 v = mul2(x, pack2(s.mul, s.mul));
-  if constexpr (FMT != FP4_MX_NVFP4) return v;
-  const f32x2 inv = pack2(s.inv, s.inv), neg = pack2(-s.s, -s.s);
-  const f32x2 q = mul2(v, inv);
-  return fma2(fma2(q, neg, v), inv, q);
+  const f32x2 mul = pack2(s.mul, s.mul), q = mul2(x, mul);
+  if constexpr (FMT != FP4_MX_NVFP4) return q;
+  // (the powers of two are kept out of nothing's range: k from -100 to 117, s from 2^-9 to 448; the remainder of a value that a code other
+  // than 0 stands for is at least 2^-139)
+  return fma2(fma2(q, pack2(-s.s, -s.s), x), mul, q);
+}
+__device__ __forceinline__ f32x2 within(f32x2 v, float most) {
+  float a, b;
+  unpack2(v, a, b);
+  return pack2(fminf(fmaxf(a, -most), most), fminf(fmaxf(b, -most), most));
 }
 // Codes of one block of N elements, pair(i) being elements 2 i and 2 i + 1.  (A block with an infinity or a NaN: 0.)
 template <int FMT, int N, class Pair>
@@ -197,6 +214,16 @@ __device__ __forceinline__ void encode_block(const Scale& s, Pair pair, uint32_t
 #pragma unroll
     for (int i = 0; i < N / 8; ++i) {
       const f32x2 v[4] = {scaled<FMT>(pair(4 * i), s), scaled<FMT>(pair(4 * i + 1), s), scaled<FMT>(pair(4 * i + 2), s), scaled<FMT>(pair(4 * i + 3), s)};
+      out[i] = e2m1_word(v);
+    }
+  }
+  if (FMT == FP4_MX_NVFP4 && s.far) {
+    // quotients that could overflow, and their remainders with them: from values that saturate all the same
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+      f32x2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = scaled<FMT>(within(pair(4 * i + k), 8.0f * s.s), s);
       out[i] = e2m1_word(v);
     }
   }
@@ -255,12 +282,12 @@ __host__ __device__ constexpr int scale_tile_bytes(int fmt) { return fmt == FP4_
 
 // Codes of a run of 32 elements into the staged codes of the tile (row r of 64 or 128 bytes), its scales among the tile's.
 template <class T, int FMT, class Pair, class Amax>
-__device__ __forceinline__ void encode_run(int r, int run, float inv_tensor, Pair pair, Amax amax, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+__device__ __forceinline__ void encode_run(int r, int run, float2 tensor, Pair pair, Amax amax, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
   constexpr int N = mx_block(FMT), BLOCKS = 32 / N;
   uint32_t w[code_words(FMT)];
 #pragma unroll
   for (int b = 0; b < BLOCKS; ++b) {
-    const Scale s = scale_of<T, FMT>(amax(b * N, N), inv_tensor);
+    const Scale s = scale_of<T, FMT>(amax(b * N, N), tensor);
     bad |= !s.finite;
     s_scale[scale_at(r, run * BLOCKS + b)] = uint8_t(s.byte);
     encode_block<FMT, N>(s, [&](int i) { return pair(b * (N / 2) + i); }, w + b * (code_words(FMT) / BLOCKS));
@@ -275,7 +302,7 @@ __device__ __forceinline__ void encode_run(int r, int run, float inv_tensor, Pai
 // E4M3 codes of a run into staged codes of 64 columns (two runs), 64-byte rows.
 template <class T>
 __device__ __forceinline__ void keep_run(const Run<T>& v, int r, int run, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
-  const Scale s = scale_of<T, FP4_MX_E4M3>(v.amax(0, 32), 1.0f);
+  const Scale s = scale_of<T, FP4_MX_E4M3>(v.amax(0, 32), NO_TENSOR_SCALE);
   bad |= !s.finite;
   s_scale[scale_at(r, run)] = uint8_t(s.byte);
   uint32_t w[8];
@@ -285,13 +312,13 @@ __device__ __forceinline__ void keep_run(const Run<T>& v, int r, int run, uint8_
 }
 // Blocks along the rows: the thread's run.
 template <class T, int FMT>
-__device__ __forceinline__ void encode_along(const Run<T>& v, int r, int run, float inv_tensor, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
-  encode_run<T, FMT>(r, run, inv_tensor, [&](int i) { return v.pair(i); }, [&](int first, int n) { return v.amax(first, n); }, s_codes, s_scale, bad);
+__device__ __forceinline__ void encode_along(const Run<T>& v, int r, int run, float2 tensor, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+  encode_run<T, FMT>(r, run, tensor, [&](int i) { return v.pair(i); }, [&](int first, int n) { return v.amax(first, n); }, s_codes, s_scale, bad);
 }
 // Blocks along the columns: thread t takes columns 2 p and 2 p + 1 (p = t % 64) of rows 32 b .. 32 b + 31 (b = t / 64).  Row `column`
 // of the staged codes holds a column's.
 template <class T, int FMT>
-__device__ __forceinline__ void encode_across(const uint8_t* tile, float inv_tensor, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
+__device__ __forceinline__ void encode_across(const uint8_t* tile, float2 tensor, uint8_t* s_codes, uint8_t* s_scale, bool& bad) {
   const int p = threadIdx.x & 63, b = threadIdx.x >> 6;
   uint32_t a[32], c[sizeof(T) == 4 ? 32 : 1];              // 16 bits: both columns in a
 #pragma unroll
@@ -325,7 +352,7 @@ __device__ __forceinline__ void encode_across(const uint8_t* tile, float inv_ten
       else return col ? TypeOf<T>::hi(a[i]) : TypeOf<T>::lo(a[i]);
     };
     const uint32_t m0 = col ? mc[0] : ma[0], m1 = col ? mc[1] : ma[1];
-    encode_run<T, FMT>(2 * p + col, b, inv_tensor, [&](int i) { return pack2(value(2 * i), value(2 * i + 1)); },
+    encode_run<T, FMT>(2 * p + col, b, tensor, [&](int i) { return pack2(value(2 * i), value(2 * i + 1)); },
                        [&](int first, int n) { return n == 32 ? max(m0, m1) : first ? m1 : m0; }, s_codes, s_scale, bad);
   }
 }
@@ -349,32 +376,97 @@ __device__ __forceinline__ void request_tile(const Side& s, Loader* l, uint8_t* 
 #pragma unroll
   for (int i = 0; i < tile_bytes<T>() / BOX_BYTES; ++i) tma_load_2d(tile + i * BOX_BYTES, &s.map, &l->bar, int(col0) + i * PER, int(row0));
 }
+// Rows off 16-byte boundaries, in: a lane takes 16 bytes of the tile's row, from the two aligned pieces that hold them, shifted into
+// place; what would touch bytes outside of the matrix, and the row's last piece, goes element by element.
 template <class T>
 __device__ __forceinline__ void copy_tile_in(const Side& s, uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
-  // 16 rows of a warp, 32 neighbouring elements at a time, eight such on their way together
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int E = int(sizeof(T)), PER = 16 / E, UNITS = MX_TILE / PER, STEPS = MX_TILE * UNITS / THREADS, AT_ONCE = 4;
+  const uintptr_t first = reinterpret_cast<uintptr_t>(s.p), last = first + uintptr_t(((rows - 1) * s.ld + cols) * E);
+  const int unit = threadIdx.x % UNITS;
+  const int64_t col = col0 + unit * PER;
 #pragma unroll 1
-  for (int i0 = 0; i0 < 64; i0 += 8) {
-    T v[8];
+  for (int i0 = 0; i0 < STEPS; i0 += AT_ONCE) {
+    uint4 lo[AT_ONCE], hi[AT_ONCE];
+    int how[AT_ONCE];                                      // shift in bytes; -1: element by element
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t r = row0 + warp * 16 + ((i0 + j) >> 2), c = col0 + ((i0 + j) & 3) * 32 + lane;
-      if (r < rows && c < cols) v[j] = static_cast<const T*>(s.p)[r * s.ld + c];
-      else v[j] = T(0.0f);
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int64_t row = row0 + (i0 + j) * (THREADS / UNITS) + threadIdx.x / UNITS;
+      lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
+      how[j] = 0;
+      if (row < rows && col < cols) {
+        const uintptr_t at = first + uintptr_t((row * s.ld + col) * E), piece = at & ~uintptr_t(15);
+        how[j] = int(at - piece);
+        if (col + PER > cols || piece < first || piece + (how[j] ? 32 : 16) > last) {
+          how[j] = -1;
+        } else {
+          lo[j] = *reinterpret_cast<const uint4*>(piece);
+          if (how[j]) hi[j] = *reinterpret_cast<const uint4*>(piece + 16);
+        }
+      }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<T*>(tile + at128(warp * 16 + ((i0 + j) >> 2), (((i0 + j) & 3) * 32 + lane) * int(sizeof(T)))) = v[j];
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = (i0 + j) * (THREADS / UNITS) + threadIdx.x / UNITS;
+      uint32_t w[8] = {lo[j].x, lo[j].y, lo[j].z, lo[j].w, hi[j].x, hi[j].y, hi[j].z, hi[j].w};
+      if (how[j] < 0) {
+        const T* p = static_cast<const T*>(s.p) + (row0 + r) * s.ld + col;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          uint32_t bits = 0;
+          if (col + i < cols) bits = E == 4 ? *reinterpret_cast<const uint32_t*>(p + i) : *reinterpret_cast<const unsigned short*>(p + i);
+          if (E == 4) w[i] = bits;
+          else w[i / 2] = i % 2 ? w[i / 2] | (bits << 16) : bits;
+        }
+        how[j] = 0;
+      }
+      const bool two = how[j] & 8, one = how[j] & 4;
+#pragma unroll
+      for (int i = 0; i < 6; ++i) w[i] = two ? w[i + 2] : w[i];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) w[i] = one ? w[i + 1] : w[i];
+      if (E == 2) {
+        const int bits = (how[j] & 3) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+      }
+      *reinterpret_cast<uint4*>(tile + at128(r, unit * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
 }
+// The same, out: whole aligned pieces of 16 bytes from where in the tile's row they lie, then what is left of a row at either end.
 template <class T>
 __device__ __forceinline__ void copy_tile_out(const Side& s, const uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll 8
-  for (int i = 0; i < 64; ++i) {
-    const int64_t r = row0 + warp * 16 + (i >> 2), c = col0 + (i & 3) * 32 + lane;
-    if (r < rows && c < cols)
-      static_cast<T*>(s.p)[r * s.ld + c] = *reinterpret_cast<const T*>(tile + at128(warp * 16 + (i >> 2), ((i & 3) * 32 + lane) * int(sizeof(T))));
+  constexpr int E = int(sizeof(T)), PER = 16 / E, UNITS = MX_TILE / PER, STEPS = MX_TILE * UNITS / THREADS;
+  const int width = int(cols - col0 < MX_TILE ? cols - col0 : MX_TILE) * E, unit = threadIdx.x % UNITS;
+#pragma unroll 2
+  for (int i = 0; i < STEPS; ++i) {
+    const int r = i * (THREADS / UNITS) + threadIdx.x / UNITS;
+    if (row0 + r >= rows) break;
+    uint8_t* out = reinterpret_cast<uint8_t*>(static_cast<T*>(s.p) + (row0 + r) * s.ld + col0);
+    const int head = int(-reinterpret_cast<intptr_t>(out) & 15), at = head + 16 * unit;      // bytes
+    if (at + 16 <= width) {
+      uint32_t w[5];
+#pragma unroll
+      for (int k = 0; k < 5; ++k) w[k] = k < 4 || (at & 3) ? *reinterpret_cast<const uint32_t*>(tile + at128(r, (at & ~3) + 4 * k)) : 0u;
+      if (E == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], (at & 3) * 8);
+      }
+      *reinterpret_cast<uint4*>(out + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  // up to PER - 1 elements at either end: 16 lanes a row
+  const int lane = threadIdx.x & 15;
+#pragma unroll 2
+  for (int r = threadIdx.x / 16; r < MX_TILE; r += THREADS / 16) {
+    if (row0 + r >= rows) break;
+    uint8_t* out = reinterpret_cast<uint8_t*>(static_cast<T*>(s.p) + (row0 + r) * s.ld + col0);
+    int head = int(-reinterpret_cast<intptr_t>(out) & 15);
+    if (head > width) head = width;
+    const int body = (width - head) & ~15;
+    const int at = lane * E < head ? lane * E : lane * E + body;             // elements [0, head) and [head + body, width)
+    if (at < width && lane * E < width - body)
+      *reinterpret_cast<T*>(out + at) = *reinterpret_cast<const T*>(tile + at128(r, at));
   }
 }
 template <class T>
@@ -407,12 +499,100 @@ struct Codes {
   bool on;
 };
 
+// The largest of the block's values, in every thread.
+__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* s_max) {
+  m = __reduce_max_sync(0xFFFFFFFFu, m);
+  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+  m = s_max[0];
+#pragma unroll
+  for (int i = 1; i < THREADS / 32; ++i) m = max(m, s_max[i]);
+  return m;
+}
+
+// ------------------------------------------------------------------ a tensor's amax (NVFP4) ---
+// Largest magnitude of a matrix as a pattern of fp32, for the block that calls.  Warps `warp`, `warp + warps`, ... take pieces of a row in
+// 16-byte loads, AT_ONCE a lane on their way together; what lies outside of whole aligned pieces goes element by element.  (Maxima of
+// integers: their order does not matter.)
+struct AmaxArgs {
+  const void* x;
+  int64_t rows, cols, ld;
+  uint32_t* parts;             // one value a block
+  uint32_t* amax;              // not null: the block that ends last joins the parts here (`ticket`, 0 between calls, tells it)
+  uint32_t* ticket;
+};
+template <class T>
+__device__ __forceinline__ uint32_t amax_of(const AmaxArgs& a, int64_t warp, int64_t warps, uint32_t* s_max) {
+  constexpr int E = int(sizeof(T)), AT_ONCE = 8;
+  constexpr int64_t PIECE = 32 * AT_ONCE * 16;                               // bytes
+  const int lane = threadIdx.x & 31;
+  const auto element = [](uintptr_t p) -> uint32_t {
+    return E == 4 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const unsigned short*>(p);
+  };
+  uint32_t m = 0;
+  const int64_t pieces = (a.cols * E + PIECE - 1) / PIECE;
+  for (int64_t row = warp / pieces, piece = warp % pieces; row < a.rows;) {
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(a.x) + uintptr_t(row * a.ld * E), end = begin + uintptr_t(a.cols * E);
+    uintptr_t body = (begin + 15) & ~uintptr_t(15), tail = end & ~uintptr_t(15);
+    if (body > end) body = end;
+    if (tail < body) tail = body;
+    const uintptr_t p = body + uintptr_t(piece * PIECE) + 16 * lane;
+    uint4 q[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      q[i] = p + 512 * i < tail ? __ldg(reinterpret_cast<const uint4*>(p + 512 * i)) : make_uint4(0, 0, 0, 0);
+    if (piece == 0) {                                      // up to 16 / E - 1 elements at either end
+      if (begin + lane * E < body) m = TypeOf<T>::most(m, element(begin + lane * E));
+      if (tail + lane * E < end) m = TypeOf<T>::most(m, element(tail + lane * E));
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      m = TypeOf<T>::most(m, TypeOf<T>::most(TypeOf<T>::most(q[i].x, q[i].y), TypeOf<T>::most(q[i].z, q[i].w)));
+    piece += warps;
+    if (piece >= pieces) {
+      row += piece / pieces;
+      piece %= pieces;
+    }
+  }
+  if constexpr (E == 2) m = max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+  else m &= 0x7FFFFFFFu;
+  return block_max(__float_as_uint(TypeOf<T>::value(m)), s_max);
+}
+template <class T>
+__global__ void __launch_bounds__(THREADS) mx_amax_kernel(const __grid_constant__ AmaxArgs a) {
+  __shared__ uint32_t s_max[THREADS / 32];
+  mx_wait_for_inputs();
+  mx_let_next_start();
+  const uint32_t m = amax_of<T>(a, int64_t(blockIdx.x) * (THREADS / 32) + (threadIdx.x >> 5), int64_t(gridDim.x) * (THREADS / 32), s_max);
+  if (threadIdx.x == 0) a.parts[blockIdx.x] = m;
+  if (!a.amax) return;
+  __shared__ bool last;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!last) return;
+  uint32_t all = 0;
+  for (unsigned i = threadIdx.x; i < gridDim.x; i += THREADS) all = max(all, *const_cast<volatile uint32_t*>(a.parts + i));
+  all = block_max(all, s_max);
+  if (threadIdx.x == 0) {
+    *a.amax = all;
+    *a.ticket = 0;
+  }
+}
+
 // -------------------------------------------------------------------------- quantisation ---
 struct QuantArgs {
   Side x;
   Codes along, across;         // blocks along the rows, along the columns
   int64_t rows, cols;
-  const uint32_t* amax;        // NVFP4
+  // NVFP4: the tensor's amax is there (no parts), is the largest of `parts` values, or (parts < 0) is found by every block for itself, which a
+  // tensor that small costs least; the first block notes it then
+  uint32_t* amax;
+  const uint32_t* part;
+  int parts;
   int32_t* status;
 };
 template <class T, int FMT, bool ROWS, bool COLS>
@@ -441,16 +621,33 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
   } else {
     copy_tile_in<T>(a.x, tile, row0, col0, a.rows, a.cols);
   }
-  const float inv_tensor = FMT == FP4_MX_NVFP4 ? pow2_int(-mx_tensor_exponent(*a.amax)) : 1.0f;
+  float2 tensor = make_float2(1.0f, 1.0f);               // 2^k, 2^-k
+  if (FMT == FP4_MX_NVFP4) {
+    __shared__ uint32_t s_max[THREADS / 32];
+    uint32_t m;
+    if (a.parts > 0) {
+      m = 0;
+      for (int i = threadIdx.x; i < a.parts; i += THREADS) m = max(m, a.part[i]);
+      m = block_max(m, s_max);
+    } else if (a.parts < 0) {
+      const AmaxArgs all = {a.x.p, a.rows, a.cols, a.x.ld, nullptr, nullptr, nullptr};
+      m = amax_of<T>(all, threadIdx.x >> 5, THREADS / 32, s_max);
+    } else {
+      m = *a.amax;
+    }
+    if (a.parts && blockIdx.x == 0 && threadIdx.x == 0) *a.amax = m;
+    const int k = mx_tensor_exponent(m);
+    tensor = make_float2(pow2_int(k), pow2_int(-k));
+  }
   __syncthreads();
   if (a.x.wide && !mbar_wait(&l.bar, 0, &l.abort, a.status)) return;      // (a copy that never comes: nothing is written)
   bool bad = false;
   if (ROWS) {
     const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) encode_along<T, FMT>(load_run<T>(tile, r, run0 + i), r, run0 + i, inv_tensor, s_along, s_scale[0], bad);
+    for (int i = 0; i < 2; ++i) encode_along<T, FMT>(load_run<T>(tile, r, run0 + i), r, run0 + i, tensor, s_along, s_scale[0], bad);
   }
-  if (COLS) encode_across<T, FMT>(tile, inv_tensor, s_across, s_scale[1], bad);
+  if (COLS) encode_across<T, FMT>(tile, tensor, s_across, s_scale[1], bad);
   fence_async_smem();
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -462,79 +659,6 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
   if (COLS) copy_scales(a.across.scales + (at.col * a.across.tiles + at.row) * BYTES, s_scale[1], BYTES);
   report(bad, a.status);
   if (threadIdx.x == 0) tma_store_wait_all();
-}
-
-// Largest magnitude of a tensor as a pattern of fp32 (integer maxima: the order of the blocks does not matter).  `wide`: rows on 16-byte
-// boundaries; 16 bytes a lane, eight such on their way together.
-struct AmaxArgs {
-  const void* x;
-  int64_t rows, cols, ld;
-  bool wide;
-  uint32_t* amax;
-};
-template <class T>
-__global__ void __launch_bounds__(THREADS) mx_amax_kernel(const AmaxArgs a) {
-  mx_wait_for_inputs();
-  mx_let_next_start();
-  constexpr int PER = 16 / int(sizeof(T)), AT_ONCE = 8;
-  uint32_t m = 0;
-  const int lane = threadIdx.x & 31;
-  // a warp walks along rows, in pieces of 32 x AT_ONCE loads
-  const int64_t warps = int64_t(gridDim.x) * (THREADS / 32), warp = int64_t(blockIdx.x) * (THREADS / 32) + (threadIdx.x >> 5);
-  const int64_t piece = a.wide ? 32 * AT_ONCE * PER : 32 * AT_ONCE, pieces = (a.cols + piece - 1) / piece;
-  for (int64_t row = warp / pieces, p = warp % pieces; row < a.rows;) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ld;
-    const int64_t c0 = p * piece;
-    if (a.wide) {
-      uint4 q[AT_ONCE];
-#pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) {
-        const int64_t c = c0 + (i * 32 + lane) * PER;
-        q[i] = make_uint4(0, 0, 0, 0);
-        if (c + PER <= a.cols) q[i] = __ldg(reinterpret_cast<const uint4*>(x + c));
-        else if (c < a.cols) {                             // the row's last, partial 16 bytes
-          uint32_t w[4] = {0, 0, 0, 0};
-          for (int j = 0; j < PER; ++j)
-            if (c + j < a.cols) {
-              if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(x[c + j]);
-              else w[j / 2] |= uint32_t(*reinterpret_cast<const unsigned short*>(x + c + j)) << (16 * (j & 1));
-            }
-          q[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i)
-        m = TypeOf<T>::most(m, TypeOf<T>::most(TypeOf<T>::most(q[i].x, q[i].y), TypeOf<T>::most(q[i].z, q[i].w)));
-    } else {
-      uint32_t v[AT_ONCE];
-#pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) {
-        const int64_t c = c0 + i * 32 + lane;
-        v[i] = 0;
-        if (c < a.cols) {
-          if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(x[c]);
-          else v[i] = *reinterpret_cast<const unsigned short*>(x + c);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) m = TypeOf<T>::most(m, v[i]);
-    }
-    p += warps;
-    if (p >= pieces) {
-      row += p / pieces;
-      p %= pieces;
-    }
-  }
-  if constexpr (sizeof(T) == 2) m = max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
-  else m &= 0x7FFFFFFFu;
-  m = __reduce_max_sync(0xFFFFFFFFu, m);
-  __shared__ uint32_t s[THREADS / 32];
-  if (lane == 0) s[threadIdx.x >> 5] = m;
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    m = __reduce_max_sync(0xFFFFFFFFu, threadIdx.x < THREADS / 32 ? s[threadIdx.x] : 0u);
-    if (threadIdx.x == 0 && m) atomicMax(a.amax, __float_as_uint(TypeOf<T>::value(m)));
-  }
 }
 
 // ------------------------------------------------------------------------ dequantisation ---
@@ -657,7 +781,7 @@ template <class T>
 __device__ __forceinline__ void finish_h(const SwigluArgs& a, const TileAt& at, uint8_t* tile, uint8_t* s_along, uint8_t* s_across,
                                          uint8_t (*s_scale)[512], bool& bad) {
   const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
-  if (a.across.on) encode_across<T, FP4_MX_E2M1>(tile, 1.0f, s_across, s_scale[1], bad);
+  if (a.across.on) encode_across<T, FP4_MX_E2M1>(tile, NO_TENSOR_SCALE, s_across, s_scale[1], bad);
   fence_async_smem();
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -724,7 +848,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd
       g.set_pair(k, g0 * sigmoid(g0).s * u[i].get(2 * k), g1 * sigmoid(g1).s * u[i].get(2 * k + 1));
     }
     if (a.has_h || a.across.on) store_run(tile, r, run, g);
-    if (a.along.on) encode_along<T, FP4_MX_E2M1>(g, r, run, 1.0f, s_along, s_scale[0], bad);
+    if (a.along.on) encode_along<T, FP4_MX_E2M1>(g, r, run, NO_TENSOR_SCALE, s_along, s_scale[0], bad);
   }
   if (a.across.on) __syncthreads();
   finish_h<T>(a, at, tile, s_along, s_across, s_scale, bad);
@@ -812,7 +936,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_sw
     store_run(t_up, r, run, e);
     if (H) {
       if (a.has_h || a.across.on) store_run(t_h, r, run, h);
-      if (a.along.on) encode_along<T, FP4_MX_E2M1>(h, r, run, 1.0f, s_along, s_scale[0], bad);
+      if (a.along.on) encode_along<T, FP4_MX_E2M1>(h, r, run, NO_TENSOR_SCALE, s_along, s_scale[0], bad);
     }
   }
   fence_async_smem();
@@ -890,14 +1014,28 @@ int quantize_as(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a) {
   return launch_tiles<mx_quantize_kernel<T, FMT, true, false>>(ctx, a.rows, a.cols, one, one, stream, a);
 }
 template <class T>
-int quantize_from(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a, const fp4_mx_tensor& q) {
+int quantize_from(fp4_ctx* ctx, cudaStream_t stream, QuantArgs a, const fp4_mx_tensor& q) {
   if (q.format == FP4_MX_NVFP4 && !(q.flags & FP4_MX_AMAX_GIVEN)) {
-    FP4_CUDA_TRY(cudaMemsetAsync(q.amax, 0, sizeof(float), stream));
-    const AmaxArgs m = {a.x.p, a.rows, a.cols, a.x.ld, a.x.wide, reinterpret_cast<uint32_t*>(q.amax)};
-    const int64_t piece = a.x.wide ? 256 * 16 / int(sizeof(T)) : 256, n = (a.rows * ((a.cols + piece - 1) / piece) + 7) / 8, most = int64_t(ctx->num_sms) * 4;
-    KernelScope scope(ctx, stream, KC_ABSMAX, 1);
-    const int rc = mx_launch<mx_amax_kernel<T>>(dim3(unsigned(n < most ? n : most)), THREADS, 0, 1, stream, m);
-    if (rc != FP4_OK) return rc;
+    // Rows without a gap are one long row.
+    const bool dense = a.x.ld == a.cols;
+    AmaxArgs m = {a.x.p, dense ? 1 : a.rows, dense ? a.rows * a.cols : a.cols, a.x.ld, ctx->mx_scratch, nullptr, nullptr};
+    const int64_t bytes = a.rows * a.cols * int64_t(sizeof(T));
+    if (bytes <= MX_SMALL_BYTES) {
+      a.parts = -1;
+    } else {
+      const int64_t n = (bytes + 8 * 4096 - 1) / (8 * 4096), most = int64_t(ctx->num_sms) * 4 < MX_SCRATCH_WORDS - 1 ? int64_t(ctx->num_sms) * 4 : MX_SCRATCH_WORDS - 1;
+      const int blocks = int(n < most ? n : most);
+      if (blocks <= MX_FEW_PARTS) {
+        a.parts = blocks;
+        a.part = ctx->mx_scratch;
+      } else {
+        m.amax = a.amax;
+        m.ticket = ctx->mx_scratch + MX_SCRATCH_WORDS - 1;
+      }
+      KernelScope scope(ctx, stream, KC_ABSMAX, 1);
+      const int rc = mx_launch<mx_amax_kernel<T>>(dim3(unsigned(blocks)), THREADS, 0, 1, stream, m);
+      if (rc != FP4_OK) return rc;
+    }
   }
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
   if (q.format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(ctx, stream, a);
@@ -940,7 +1078,7 @@ int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, MxMatrix x, int dtype,
   QuantArgs a = {};
   a.rows = q.rows;
   a.cols = q.cols;
-  a.amax = reinterpret_cast<const uint32_t*>(q.amax);
+  a.amax = reinterpret_cast<uint32_t*>(q.amax);
   a.status = status;
   int rc = matrix_side(ctx, &a.x, x, q.rows, q.cols, dtype, false);
   if (rc == FP4_OK) rc = codes_along(ctx, &a.along, q, q.rows, q.cols);

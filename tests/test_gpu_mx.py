@@ -77,6 +77,27 @@ def test_quantize(lib, ctx, fmt, dt, shape):
     assert ctx.read_status() == 0
 
 
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("cols", [1, 7, 8, 128, 137, 393])
+def test_every_alignment_of_rows(lib, ctx, dt, cols):
+    """Rows that begin at each place within 16 bytes, read and written, in matrices that begin and end where their memory does."""
+    E = torch.finfo(DT[dt]).bits // 8
+    for ld in range(cols, cols + 16 // E):
+        for first in range(0, 16 // E, 3):
+            rows = 131
+            flat = draw(1, first + (rows - 1) * ld + cols, dt, seed=ld + first)[0]
+            x = torch.as_strided(flat, (rows, cols), (ld, 1), first)
+            q = lib.fp4_mx_quantize(ctx, x, lib.FP4_MX_NVFP4, True, True)
+            check_quantized(q, x, "nvfp4")
+            before = flat.clone()
+            out = torch.as_strided(flat, (rows, cols), (ld, 1), first)
+            lib.fp4_mx_dequantize(ctx, q, out=out)
+            want = torch.from_numpy(O.quantize(host(torch.as_strided(before, (rows, cols), (ld, 1), first)), "nvfp4").values).to(DT[dt])
+            assert torch.equal(out.cpu(), want)
+            torch.as_strided(before, (rows, cols), (ld, 1), first).copy_(out)
+            assert torch.equal(before, flat)                          # nothing beside the matrix was written
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
 def test_quantize_strided_input(lib, ctx, fmt, dt):
@@ -148,6 +169,36 @@ def test_given_amax(lib, ctx):
         q = lib.fp4_mx_quantize(ctx, x, lib.FP4_MX_NVFP4, True, True, amax=torch.tensor([a], device="cuda"))
         assert float(q.amax.item()) == np.float32(a)
         check_quantized(q, x, "nvfp4", amax=float(np.float32(a)))
+
+
+def test_given_amax_far_below_the_values(lib, ctx):
+    """Saturation, with the values' signs, however far beyond: quotients that overflow fp32 among them."""
+    x = draw(40, 96, "bf16", seed=12)
+    x[3, 10], x[3, 11], x[20, 40], x[21, 41] = 3e38, -3e38, 1e30, -1e20
+    for a in (0.0, 1e-37, 1e-20, 1.0):
+        q = lib.fp4_mx_quantize(ctx, x, lib.FP4_MX_NVFP4, True, True, amax=torch.tensor([a], device="cuda"))
+        check_quantized(q, x, "nvfp4", amax=float(np.float32(a)))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("k", [-100, -37, 0, 40, 110])
+def test_every_tie_of_blocks_of_16(lib, ctx, dt, k):
+    """Every E4M3 scale with every value that lies on a tie of E2M1 under it, and its neighbours in the type, at several scales of the tensor."""
+    mids = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    s = O.E4M3[1:]                                                    # every scale but 0
+    x = np.zeros((2 * len(s), 32))
+    for i, v in enumerate(s):
+        ties = mids * v * 2.0 ** k
+        x[2 * i, :7], x[2 * i, 7:14] = ties, -ties
+        x[2 * i, 14] = x[2 * i + 1, 14] = 6.0 * v * 2.0 ** k          # the block's amax: its scale is v
+        t = torch.tensor(ties).to(DT[dt])
+        inf = torch.tensor(float("inf"), dtype=DT[dt])
+        x[2 * i + 1, :7], x[2 * i + 1, 7:14] = torch.nextafter(t, inf).double(), -torch.nextafter(t, -inf).double()
+    t = torch.tensor(x).to(DT[dt]).cuda()
+    if dt == "fp32" or k > -90:
+        assert np.array_equal(host(t)[::2], x[::2])                   # the ties are values of the type
+    q = lib.fp4_mx_quantize(ctx, t, lib.FP4_MX_NVFP4, True, True, amax=torch.tensor([2688.0 * 2.0 ** k], device="cuda"))
+    check_quantized(q, t, "nvfp4", amax=2688.0 * 2.0 ** k)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
