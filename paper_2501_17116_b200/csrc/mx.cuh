@@ -80,7 +80,13 @@ struct MxMatrix {               // a matrix of the caller's: rows of `ld` elemen
   int64_t ld;
 };
 
-int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, MxMatrix x, int dtype, const fp4_mx_tensor& q, int32_t* status);
+// One tensor or two, neither empty.
+struct MxQuantize {
+  MxMatrix x;
+  int dtype;
+  const fp4_mx_tensor* q;
+};
+int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize* what, int n, int32_t* status);
 int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes, const uint8_t* scales, const float* amax,
                          int64_t rows, int64_t cols, int format, MxMatrix out, int dtype, int32_t* status);
 // `h` may have no pointer; `q` (may be null): E2M1 in blocks of 32.
@@ -102,4 +108,5 @@ struct MxGemm {
   int dtype;
   bool accumulate;
 };
-int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* status);
+// One product or two that do not depend on one another, none of them empty.
+int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, int32_t* status);

@@ -54,26 +54,51 @@ int check_tensor(const fp4_mx_tensor* q, bool e2m1_only) {
   return rc;
 }
 
-int quantize(fp4_ctx* ctx, cudaStream_t st, const fp4_mx_matrix* x, const fp4_mx_tensor& q, int32_t* status) {
-  if (q.rows == 0 || q.cols == 0) {
-    if (q.format == FP4_MX_NVFP4 && !(q.flags & FP4_MX_AMAX_GIVEN)) FP4_CUDA_TRY(cudaMemsetAsync(q.amax, 0, sizeof(float), st));
-    return FP4_OK;
+// Up to two tensors; what is empty takes no launch.
+struct Quantize {
+  const fp4_mx_matrix* x;
+  const fp4_mx_tensor* q;
+};
+int quantize(fp4_ctx* ctx, cudaStream_t st, const Quantize* what, int n, int32_t* status) {
+  MxQuantize todo[2];
+  int some = 0;
+  for (int i = 0; i < n; ++i) {
+    const fp4_mx_tensor& q = *what[i].q;
+    if (q.rows == 0 || q.cols == 0) {
+      if (q.format == FP4_MX_NVFP4 && !(q.flags & FP4_MX_AMAX_GIVEN)) FP4_CUDA_TRY(cudaMemsetAsync(q.amax, 0, sizeof(float), st));
+    } else {
+      todo[some++] = {matrix(what[i].x, q.rows, q.cols), what[i].x->dtype, &q};
+    }
   }
-  return launch_mx_quantize(ctx, st, matrix(x, q.rows, q.cols), x->dtype, q, status);
+  return some ? launch_mx_quantize(ctx, st, todo, some, status) : FP4_OK;
 }
 
-int gemm(fp4_ctx* ctx, cudaStream_t st, const fp4_mx_tensor* a, bool a_t, const fp4_mx_tensor* b, bool b_t, int64_t I, int64_t J,
-         int64_t C, const fp4_mx_matrix* out, bool accumulate, int32_t* status) {
-  if (I == 0 || J == 0) return FP4_OK;
-  const MxMatrix o = matrix(out, I, J);
-  const int64_t elt = out->dtype == FP4_DTYPE_FP32 ? 4 : 2;
-  if (C == 0) {
-    if (!accumulate) FP4_CUDA_TRY(cudaMemset2DAsync(out->data, size_t(o.ld * elt), 0, size_t(J * elt), size_t(I), st));
-    return FP4_OK;
+// a b^T over I x J results and a contraction of C, up to two.
+struct Gemm {
+  const fp4_mx_tensor* a;
+  bool a_t;
+  const fp4_mx_tensor* b;
+  bool b_t;
+  int64_t I, J, C;
+  const fp4_mx_matrix* out;
+  bool accumulate;
+};
+int gemm(fp4_ctx* ctx, cudaStream_t st, const Gemm* what, int n, int32_t* status) {
+  MxGemm todo[2];
+  int some = 0;
+  for (int i = 0; i < n; ++i) {
+    const Gemm& g = what[i];
+    if (g.I == 0 || g.J == 0) continue;
+    const MxMatrix o = matrix(g.out, g.I, g.J);
+    const int64_t elt = g.out->dtype == FP4_DTYPE_FP32 ? 4 : 2;
+    if (g.C == 0) {
+      if (!g.accumulate) FP4_CUDA_TRY(cudaMemset2DAsync(g.out->data, size_t(o.ld * elt), 0, size_t(g.J * elt), size_t(g.I), st));
+      continue;
+    }
+    todo[some++] = {g.a_t ? g.a->codes_t : g.a->codes, g.a_t ? g.a->scales_t : g.a->scales, g.b_t ? g.b->codes_t : g.b->codes,
+                    g.b_t ? g.b->scales_t : g.b->scales, g.a->amax, g.b->amax, g.I, g.J, g.C, g.a->format, g.out->data, o.ld, g.out->dtype, g.accumulate};
   }
-  const MxGemm g = {a_t ? a->codes_t : a->codes, a_t ? a->scales_t : a->scales, b_t ? b->codes_t : b->codes, b_t ? b->scales_t : b->scales,
-                    a->amax, b->amax, I, J, C, a->format, out->data, o.ld, out->dtype, accumulate};
-  return launch_mx_gemm(ctx, st, g, status);
+  return some ? launch_mx_gemm(ctx, st, todo, some, status) : FP4_OK;
 }
 
 int check_swiglu_quantized(const fp4_mx_tensor* q) {
@@ -117,7 +142,8 @@ int fp4_mx_quantize(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, fp4_mx_t
   if (rc != FP4_OK) return rc;
   OnDevice device(ctx);
   if (!device.ok) return FP4_ERR_CUDA;
-  return quantize(ctx, static_cast<cudaStream_t>(stream), x, *out, status);
+  const Quantize one = {x, out};
+  return quantize(ctx, static_cast<cudaStream_t>(stream), &one, 1, status);
 }
 
 int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int transposed, const fp4_mx_matrix* out, int32_t* status) {
@@ -157,7 +183,8 @@ int fp4_mx_gemm(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* a, const fp4_mx
   if (rc != FP4_OK) return rc;
   OnDevice device(ctx);
   if (!device.ok) return FP4_ERR_CUDA;
-  return gemm(ctx, static_cast<cudaStream_t>(stream), a, a_t, b, b_t, I, J, C, out, flags & FP4_MX_ACCUMULATE, status);
+  const Gemm one = {a, a_t, b, b_t, I, J, C, out, bool(flags & FP4_MX_ACCUMULATE)};
+  return gemm(ctx, static_cast<cudaStream_t>(stream), &one, 1, status);
 }
 
 int fp4_mx_linear_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, const fp4_mx_matrix* w, int64_t M, int64_t K, int64_t N,
@@ -183,18 +210,22 @@ int fp4_mx_linear_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, const 
   OnDevice device(ctx);
   if (!device.ok) return FP4_ERR_CUDA;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  Quantize todo[2];
+  int n = 0;
   if (!reuse_w) {
     saved_w->rows = K;
     saved_w->cols = N;
-    rc = quantize(ctx, st, w, *saved_w, status);
+    todo[n++] = {w, saved_w};
   }
-  if (rc == FP4_OK && !reuse_x) {
+  if (!reuse_x) {
     saved_x->rows = M;
     saved_x->cols = K;
-    rc = quantize(ctx, st, x, *saved_x, status);
+    todo[n++] = {x, saved_x};
   }
+  if (n) rc = quantize(ctx, st, todo, n, status);
   if (rc != FP4_OK) return rc;
-  return gemm(ctx, st, saved_x, false, saved_w, true, M, N, K, y, false, status);
+  const Gemm one = {saved_x, false, saved_w, true, M, N, K, y, false};
+  return gemm(ctx, st, &one, 1, status);
 }
 
 int fp4_mx_linear_bwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* dy, const fp4_mx_tensor* saved_x, const fp4_mx_tensor* saved_w,
@@ -236,10 +267,14 @@ int fp4_mx_linear_bwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* dy, const
   OnDevice device(ctx);
   if (!device.ok) return FP4_ERR_CUDA;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  rc = quantize(ctx, st, dy, q, status);
-  if (rc == FP4_OK && want_dx) rc = gemm(ctx, st, &q, false, saved_w, false, M, K, N, dx, flags & FP4_MX_ACCUMULATE_DX, status);
-  if (rc == FP4_OK && want_dw) rc = gemm(ctx, st, saved_x, true, &q, true, K, N, M, dw, flags & FP4_MX_ACCUMULATE_DW, status);
-  return rc;
+  const Quantize one = {dy, &q};
+  rc = quantize(ctx, st, &one, 1, status);
+  if (rc != FP4_OK) return rc;
+  Gemm todo[2];
+  int n = 0;
+  if (want_dx) todo[n++] = {&q, false, saved_w, false, M, K, N, dx, bool(flags & FP4_MX_ACCUMULATE_DX)};
+  if (want_dw) todo[n++] = {saved_x, true, &q, true, K, N, M, dw, bool(flags & FP4_MX_ACCUMULATE_DW)};
+  return gemm(ctx, st, todo, n, status);
 }
 
 int fp4_mx_swiglu_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* gate, const fp4_mx_matrix* up, int64_t rows, int64_t cols,

@@ -148,11 +148,12 @@ __device__ __forceinline__ float2 tensor_scales(const Powers& p) {
   return s;
 }
 
-// 32 rows x 32 columns (the last chunk: fewer) of a warp, row `lane` in y.  Three ways out:
+// 32 rows x 32 columns (the last ones: fewer) of a warp, row `lane` in y.  Ways out:
 //   BULK      boxes of 32 rows x 64 bytes through shared memory to the copy engine
 //   BULK_ADD  the same, what is there added first: every lane reads its row's 64 (fp32: 128) bytes
-//   ANY       any alignment: through shared memory, so that a row's values lie in a row of lanes
-enum Way { BULK = 0, BULK_ADD = 1, ANY = 2 };
+//   ANY       any alignment: rows through shared memory, from there in aligned pieces of 16 bytes
+//   ANY_ADD   the same, in fp32 to the last, with what is there added
+enum Way { BULK = 0, BULK_ADD = 1, ANY = 2, ANY_ADD = 3 };
 template <int DT>
 __device__ __forceinline__ uint32_t two_values(float a, float b) {
   if constexpr (DT == FP4_DTYPE_BF16) {
@@ -230,90 +231,216 @@ __device__ __forceinline__ void store_bulk(const float (&y)[32], uint8_t* stage,
     if (elect_one()) tma_store_2d(map, buf, col0 + 16 * u, row0);
   }
 }
+// Staged rows (32 of 128 bytes, 16-byte unit u of row r at u ^ (r & 7)) to rows of any alignment: whole aligned pieces of 16 bytes from where in
+// the staged row they lie, then what is left of a row at either end.  Several rows' loads are on their way together: two warps a scheduler
+// hide little else.  (A bulk copy of the aligned part of each row instead: 4096 x 5505 x 2048 48 us; element by element 71.)
+__device__ __forceinline__ uint32_t at_stage(int r, int byte) { return uint32_t(r * 128 + (byte ^ ((r & 7) << 4))); }
 template <int DT>
-__device__ __forceinline__ void store_any(const float (&y)[32], uint8_t* stage, const OutArgs& o, int row0, int col0, int lane) {
+__device__ __forceinline__ void send_rows(const uint8_t* stage, const OutArgs& o, int row0, int col0, int cols, int lane) {
   typedef typename OutOf<DT>::type T;
-  float* buf = reinterpret_cast<float*>(stage);
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    *reinterpret_cast<float4*>(buf + lane * 32 + ((j ^ (lane & 7)) * 4)) = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
-  __syncwarp();
-  const int rows = min(32, o.I - row0);
-  if (col0 + lane >= o.J) return;
-  T* p = static_cast<T*>(o.p) + int64_t(row0) * o.ld + col0 + lane;
-  constexpr int AT_ONCE = 8;                               // rows whose old values are on their way together
+  constexpr int E = int(sizeof(T)), AT_ONCE = 2;
+  const int rows = min(32, o.I - row0), width = min(cols, o.J - col0) * E;
+  uint8_t* out = reinterpret_cast<uint8_t*>(static_cast<T*>(o.p) + int64_t(row0) * o.ld + col0);
+  const uint32_t low = uint32_t(reinterpret_cast<uintptr_t>(out)), low_pitch = uint32_t(o.ld * E);      // (the low bits tell a row's place)
+  const int64_t pitch = o.ld * E;
+  uint8_t* p = out + (lane >> 3) * pitch;
 #pragma unroll 1
-  for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
-    float v[AT_ONCE];
+  for (int i = 0; i < 8; i += AT_ONCE) {
+    uint32_t w[AT_ONCE][5];
+    int at[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const int r = r0 + i;
-      v[i] = buf[r * 32 + (((lane >> 2) ^ (r & 7)) * 4) + (lane & 3)];
-      if (o.accumulate && r < rows) v[i] += OutOf<DT>::get(p[int64_t(r) * o.ld]);
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = 4 * (i + j) + (lane >> 3);
+      at[j] = int((0u - low - uint32_t(r) * low_pitch) & 15u) + 16 * (lane & 7);
+      if (r >= rows || at[j] + 16 > width) at[j] = -1;
+      const int word = at[j] < 0 ? 0 : at[j] & ~3;
+#pragma unroll
+      for (int k = 0; k < 5; ++k)                          // (the fifth, of a row's last piece, may lie in the next row: it is shifted out then)
+        if (k < 4 || E == 2) w[j][k] = *reinterpret_cast<const uint32_t*>(stage + at_stage(r, (word + 4 * k) & 127));
     }
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i)
-      if (r0 + i < rows) p[int64_t(r0 + i) * o.ld] = OutOf<DT>::put(v[i]);
+    for (int j = 0; j < AT_ONCE; ++j) {
+      if (E == 2)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[j][k] = __funnelshift_r(w[j][k], w[j][k + 1], (at[j] & 3) * 8);
+      if (at[j] >= 0) *reinterpret_cast<uint4*>(p + at[j]) = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
+      p += 4 * pitch;
+    }
+  }
+  // elements [0, head) and behind the last piece: of 128 bytes 16 / E together, else fewer than twice that
+  const int lanes = width == 128 ? 16 / E : 16, e = lane % lanes * E, per = 32 / lanes;
+  p = out + (lane / lanes) * pitch;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += AT_ONCE * per) {
+    T v[AT_ONCE];
+    int at[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = r0 + j * per + lane / lanes;
+      const int head = min(int((0u - low - uint32_t(r) * low_pitch) & 15u), width), body = (width - head) & ~15;
+      at[j] = e < head ? e : e + body;
+      if (r >= rows || e >= width - body) at[j] = -1;
+      v[j] = *reinterpret_cast<const T*>(stage + at_stage(r & 31, at[j] < 0 ? 0 : at[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      if (at[j] >= 0) *reinterpret_cast<T*>(p + at[j]) = v[j];
+      p += per * pitch;
+    }
+  }
+}
+// Staged rows of 32 fp32 values (16-byte unit u of row r at u ^ (r & 7)), added to rows of any alignment.
+template <int DT>
+__device__ __forceinline__ void add_rows(const uint8_t* stage, const OutArgs& o, int row0, int col0, int lane) {
+  typedef typename OutOf<DT>::type T;
+  constexpr int E = int(sizeof(T)), PER = 16 / E, UNITS = 32 / PER, AT_ONCE = 4;
+  const int rows = min(32, o.I - row0), width = min(32, o.J - col0);
+  T* out = static_cast<T*>(o.p) + int64_t(row0) * o.ld + col0;
+  const uint32_t low = uint32_t(reinterpret_cast<uintptr_t>(out)), low_pitch = uint32_t(o.ld * E);
+#pragma unroll 1
+  for (int i = 0; i < UNITS; i += AT_ONCE) {
+    uint4 q[AT_ONCE];
+    int at[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = (i + j) * (32 / UNITS) + lane / UNITS;
+      at[j] = int((0u - low - uint32_t(r) * low_pitch) & 15u) / E + PER * (lane % UNITS);
+      if (r >= rows || at[j] + PER > width) at[j] = -1;
+      if (at[j] >= 0) q[j] = *reinterpret_cast<const uint4*>(out + int64_t(r) * o.ld + at[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = (i + j) * (32 / UNITS) + lane / UNITS;
+      if (at[j] < 0) continue;
+      uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
+      float v[PER];
+#pragma unroll
+      for (int k = 0; k < PER; ++k) v[k] = *reinterpret_cast<const float*>(stage + at_stage(r, 4 * (at[j] + k)));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (PER == 4) {
+          w[k] = __float_as_uint(v[k] + __uint_as_float(w[k]));
+        } else {
+          const float2 f = two_floats<DT>(w[k]);
+          w[k] = two_values<DT>(v[2 * k] + f.x, v[2 * k + 1] + f.y);
+        }
+      }
+      *reinterpret_cast<uint4*>(out + int64_t(r) * o.ld + at[j]) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  // elements [0, head) and behind the last piece: of 32 columns PER together, else fewer than twice that
+  const int lanes = width == 32 ? PER : 16, e = lane % lanes, per = 32 / lanes;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += AT_ONCE * per) {
+    T old[AT_ONCE];
+    int at[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = r0 + j * per + lane / lanes;
+      const int head = min(int((0u - low - uint32_t(r) * low_pitch) & 15u) / E, width), body = (width - head) / PER * PER;
+      at[j] = e < head ? e : e + body;
+      if (r >= rows || e >= width - body) at[j] = -1;
+      if (at[j] >= 0) old[j] = out[int64_t(r) * o.ld + at[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int r = r0 + j * per + lane / lanes;
+      if (at[j] >= 0) out[int64_t(r) * o.ld + at[j]] = OutOf<DT>::put(*reinterpret_cast<const float*>(stage + at_stage(r, 4 * at[j])) + OutOf<DT>::get(old[j]));
+    }
   }
 }
 
-// One tile's accumulators (args.bn columns from `t_base` on) for one warp: the two warps of a lane quarter take chunks of 32 columns
-// in turn.  `free_bar`: barrier that says the accumulators may be overwritten, 0 where that is not this lane's to say.
+__device__ __forceinline__ void read_accumulators(float (&y)[32], uint32_t taddr, float2 scales) {
+  uint32_t v[32];
+  tmem_ld_32x32(taddr, v);
+  tmem_ld_wait(v);
+#pragma unroll
+  for (int k = 0; k < 32; ++k) y[k] = __uint_as_float(v[k]) * scales.x * scales.y;
+}
+// One tile's accumulators (`bn` columns from `t_base` on) for one warp: the two warps of a lane quarter take pieces of 32 columns (ANY, 16-bit
+// results: 64) in turn, those that the stages share (wide: the first stage's last ones, the second's first) ahead of the others.  `free_bar`:
+// barrier that says the accumulators may be overwritten (0: not this lane's to say).
 template <int DT, int WAY>
 __device__ __forceinline__ uint32_t store_tile(uint32_t t_base, int bn, bool wide, bool first_stage, int group, int row0, int n0, const OutArgs& o,
-                                            const CUtensorMap* map, uint8_t* stage, int lane, uint32_t seq, float2 scales,
-                                            uint32_t free_bar) {
-  const int n_valid = min(bn, o.J - n0), chunks = bn / 32;
+                                               const CUtensorMap* map, uint8_t* stage, int lane, uint32_t seq, float2 scales,
+                                               uint32_t free_bar) {
+  constexpr int COLS = WAY == ANY && DT != FP4_DTYPE_FP32 ? 64 : 32;
+  const int n_valid = min(bn, o.J - n0), pieces = bn / COLS;
+  const auto release = [&] {
+    tc_fence_before();
+    __syncwarp();
+    if (free_bar) mbar_arrive_remote(free_bar);
+  };
+  if (group >= pieces) release();
 #pragma unroll 1
-  for (int i = group; i < chunks; i += 2) {
-    // the columns that the stages share (wide: the first stage's last ones, the second's first) go ahead of the others
-    const int c = 32 * (wide && first_stage ? chunks - 1 - i : i);
+  for (int i = group; i < pieces; i += 2) {
+    const int c = COLS * (wide && first_stage ? pieces - 1 - i : i);
     const bool some = c < n_valid && row0 < o.I;
+    const bool last_read = wide ? i == group : i + 2 >= pieces;
     float y[32];
-    Old<DT> old;
-    constexpr bool EARLY = WAY == BULK_ADD && DT != FP4_DTYPE_FP32;      // (fp32: the accumulators need the registers)
-    if (EARLY && some) load_old<DT>(old, o, row0 + lane, n0 + c);
-    if (some) {
-      uint32_t v[32];
-      tmem_ld_32x32(t_base + uint32_t(c), v);
-      tmem_ld_wait(v);
-#pragma unroll
-      for (int k = 0; k < 32; ++k) y[k] = __uint_as_float(v[k]) * scales.x * scales.y;
-    }
-    if (wide ? i == group : i + 2 >= chunks) {
-      tc_fence_before();
+    if constexpr (COLS == 64) {
       __syncwarp();
-      if (free_bar) mbar_arrive_remote(free_bar);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {                        // two times 32 columns
+        if (some) read_accumulators(y, t_base + uint32_t(c + 32 * h), scales);
+        if (h == 1 && last_read) release();
+        if (some)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float* v = y + 8 * j;
+            *reinterpret_cast<uint4*>(stage + at_stage(lane, 64 * h + 16 * j)) =
+                make_uint4(two_values<DT>(v[0], v[1]), two_values<DT>(v[2], v[3]), two_values<DT>(v[4], v[5]), two_values<DT>(v[6], v[7]));
+          }
+      }
+      __syncwarp();
+      if (some) send_rows<DT>(stage, o, row0, n0 + c, 64, lane);
+    } else {
+      Old<DT> old;
+      constexpr bool EARLY = WAY == BULK_ADD && DT != FP4_DTYPE_FP32;      // (fp32: the accumulators need the registers)
+      if (EARLY && some) load_old<DT>(old, o, row0 + lane, n0 + c);
+      if (some) read_accumulators(y, t_base + uint32_t(c), scales);
+      if (last_read) release();
+      if (!some) continue;
+      if (WAY == BULK_ADD) {
+        if (!EARLY) load_old<DT>(old, o, row0 + lane, n0 + c);
+        add_old<DT>(y, old);
+      }
+      if constexpr (WAY == BULK || WAY == BULK_ADD) {
+        store_bulk<DT>(y, stage, o, map, row0, n0 + c, lane, seq);
+      } else {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          *reinterpret_cast<float4*>(stage + at_stage(lane, 16 * j)) = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+        __syncwarp();
+        if constexpr (WAY == ANY) send_rows<DT>(stage, o, row0, n0 + c, 32, lane);
+        else add_rows<DT>(stage, o, row0, n0 + c, lane);
+      }
     }
-    if (!some) continue;
-    if (WAY == BULK_ADD) {
-      if (!EARLY) load_old<DT>(old, o, row0 + lane, n0 + c);
-      add_old<DT>(y, old);
-    }
-    if (WAY == ANY) store_any<DT>(y, stage, o, row0, n0 + c, lane);
-    else store_bulk<DT>(y, stage, o, map, row0, n0 + c, lane, seq);
   }
   return seq;
 }
 
+// One product of a launch, of one or two (a second without tiles: none).
+struct Problem {
+  CUtensorMap a, b, sa, sb, out;
+  int num_k_blocks, num_m_blocks, num_n_blocks;
+  OutArgs to;
+  Powers powers;
+};
 struct GemmArgs {
-  int num_k_blocks, num_m_blocks, num_n_blocks, bn;
+  Problem p[2];
+  int bn;
   int b_tiles;                 // scale tiles of 128 rows that a tile's columns touch
   int stages, stage_bytes;
   uint32_t tx_bytes, idesc;
-  OutArgs out;
-  Powers powers;
   int32_t* status;
   uint64_t wait_limit_ns;
 };
 constexpr int FIXED_SMEM = 1024 + MISC_BYTES + EPI_WARPS * STAGE_OUT;
 
-template <int FMT, bool PAIR, int DT>
-__global__ void __launch_bounds__(THREADS, 1)
-mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
-               const __grid_constant__ CUtensorMap map_out, const __grid_constant__ GemmArgs args) {
+template <int FMT, bool PAIR, int DT, bool ALIGNED>
+__global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_constant__ GemmArgs args) {
   constexpr int CTAS = PAIR ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -331,7 +458,9 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
   const int warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
-  const int num_tiles = args.num_m_blocks * args.num_n_blocks;
+  // The tiles of the first product come first.
+  const int tiles_first = args.p[0].num_m_blocks * args.p[0].num_n_blocks;
+  const int num_tiles = tiles_first + args.p[1].num_m_blocks * args.p[1].num_n_blocks;
   const int rank = PAIR ? int(cluster_ctarank()) : 0;
   const int worker = int(blockIdx.x) / CTAS, workers = int(gridDim.x) / CTAS;
   const bool wide = args.bn > BN_TWICE;
@@ -351,21 +480,24 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     fence_async_smem();
   }
   const uint32_t full0 = PAIR ? cluster_address(full_bar, 0) : smem_u32(full_bar);      // (a pair's copies complete on the even CTA's)
-  const auto request = [&](int m_blk, int n0, int kb, int stage) {
+  const auto request = [&](const Problem& q, int m_blk, int n0, int kb, int stage) {
     uint8_t* p = smem + stage * STAGE_BYTES;
     const uint32_t bar = full0 + 8 * stage;
     if (rank == 0) mbar_arrive_expect_tx(&full_bar[stage], CTAS * args.tx_bytes);
-    tma_load_2d_group<CTAS>(p, &map_a, bar, kb * 128, m_blk * BM);
-    tma_load_2d_group<CTAS>(p + A_BYTES, &map_b, bar, kb * 128, n0 + rank * (args.bn / CTAS));
-    tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes, &map_sa, bar, kb * (scale_bytes(FMT) / 8), m_blk);
-    tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes + scale_bytes(FMT), &map_sb, bar, kb * (scale_bytes(FMT) / 8), n0 / 128);
+    tma_load_2d_group<CTAS>(p, &q.a, bar, kb * 128, m_blk * BM);
+    tma_load_2d_group<CTAS>(p + A_BYTES, &q.b, bar, kb * 128, n0 + rank * (args.bn / CTAS));
+    tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes, &q.sa, bar, kb * (scale_bytes(FMT) / 8), m_blk);
+    tma_load_2d_group<CTAS>(p + A_BYTES + b_bytes + scale_bytes(FMT), &q.sb, bar, kb * (scale_bytes(FMT) / 8), n0 / 128);
   };
   if (warp == 1) tmem_alloc<CTAS>(tmem_slot, TMEM_COLS);
   mx_wait_for_inputs();
   // Single CTAs: the stages are empty and the barriers this thread's own work, so the first tile's first k-blocks travel while the
   // others meet.  (A pair's barriers have to be known to exist first.)
-  if (!PAIR && threadIdx.x == 0 && worker < num_tiles)
-    for (int s = 0; s < STAGES && s < args.num_k_blocks; ++s) request(worker % args.num_m_blocks, worker / args.num_m_blocks * args.bn, s, s);
+  if (!PAIR && threadIdx.x == 0 && worker < num_tiles) {
+    const Problem& q = args.p[worker >= tiles_first];
+    const int tt = worker - (worker >= tiles_first ? tiles_first : 0);
+    for (int s = 0; s < STAGES && s < q.num_k_blocks; ++s) request(q, tt % q.num_m_blocks, tt / q.num_m_blocks * args.bn, s, s);
+  }
   tc_fence_before();
   __syncthreads();
   mx_let_next_start();
@@ -380,12 +512,14 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       uint32_t phase = 0, fills = 0;
       bool ok = true;
       for (int t = worker; t < num_tiles && ok; t += workers) {
-        const int m_blk = CTAS * (t % args.num_m_blocks) + rank, n0 = (t / args.num_m_blocks) * args.bn;
-        for (int kb = 0; kb < args.num_k_blocks; ++kb) {
+        const Problem& q = args.p[t >= tiles_first];
+        const int tt = t - (t >= tiles_first ? tiles_first : 0);
+        const int m_blk = CTAS * (tt % q.num_m_blocks) + rank, n0 = (tt / q.num_m_blocks) * args.bn;
+        for (int kb = 0; kb < q.num_k_blocks; ++kb) {
           if (PAIR || t != worker || kb >= STAGES) {            // (those are on their way)
             ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
             if (!ok) break;
-            request(m_blk, n0, kb, stage);
+            request(q, m_blk, n0, kb, stage);
           }
           ++fills;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -422,13 +556,15 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       for (int t = worker; t < num_tiles && ok; t += workers, ++n) {
         const int acc = n & 1;
         const uint32_t d_tmem = tmem_base + uint32_t(acc * acc_offset(FMT, wide));
-        const int shift = (t / args.num_m_blocks) * args.bn % 128 ? 2 : 0;
+        const Problem& q = args.p[t >= tiles_first];
+        const int shift = (t - (t >= tiles_first ? tiles_first : 0)) / q.num_m_blocks * args.bn % 128 ? 2 : 0;
+        const int num_k_blocks = q.num_k_blocks;
         // A stage is free when the tile before the last has left it.  Wide: when the last has left the columns that both stages have.
         const int back = wide ? 1 : 2;
         ok = n < back || mbar_wait(&acc_empty[(n - back) & 1], uint32_t((n - back) >> 1) & 1u, abort_flag, args.status, args.wait_limit_ns);
         if (!ok) break;
         tc_fence_after();
-        for (int kb = 0; kb < args.num_k_blocks; ++kb) {
+        for (int kb = 0; kb < num_k_blocks; ++kb) {
           ok = mbar_wait(&full_bar[stage], phase, abort_flag, args.status, args.wait_limit_ns);
           if (!ok) break;
           tc_fence_after();
@@ -459,22 +595,22 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     int acc = 0;
     uint32_t acc_phase = 0, seq = 0;
     const uint32_t acc_empty0 = PAIR ? cluster_address(acc_empty, 0) : smem_u32(acc_empty);
-    const float2 scales = tensor_scales(args.powers);
-    const int way = !args.out.bulk ? ANY : args.out.accumulate ? BULK_ADD : BULK;
     for (int t = worker; t < num_tiles; t += workers) {
-      const int m_blk = CTAS * (t % args.num_m_blocks) + rank, n0 = (t / args.num_m_blocks) * args.bn;
+      const Problem& q = args.p[t >= tiles_first];
+      const int tt = t - (t >= tiles_first ? tiles_first : 0);
+      const int m_blk = CTAS * (tt % q.num_m_blocks) + rank, n0 = (tt / q.num_m_blocks) * args.bn;
+      const float2 scales = tensor_scales(q.powers);
       if (!__all_sync(0xFFFFFFFFu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, args.status, args.wait_limit_ns))) break;
       tc_fence_after();
       const uint32_t t_base = tmem_base + (uint32_t(quarter * 32) << 16) + uint32_t(acc * acc_offset(FMT, wide));
       const int row0 = m_blk * BM + quarter * 32;
       const uint32_t free_bar = lane == 0 ? acc_empty0 + 8 * acc : 0u;
       const auto store = [&](auto the_way) {
-        seq = store_tile<DT, decltype(the_way)::value>(t_base, args.bn, wide, acc == 0, group, row0, n0, args.out, &map_out, stage, lane, seq,
+        seq = store_tile<DT, decltype(the_way)::value>(t_base, args.bn, wide, acc == 0, group, row0, n0, q.to, &q.out, stage, lane, seq,
                                                        scales, free_bar);
       };
-      if (way == BULK) store(std::integral_constant<int, BULK>());
-      else if (way == BULK_ADD) store(std::integral_constant<int, BULK_ADD>());
-      else store(std::integral_constant<int, ANY>());
+      if (q.to.accumulate) store(std::integral_constant<int, ALIGNED ? BULK_ADD : ANY_ADD>());
+      else store(std::integral_constant<int, ALIGNED ? BULK : ANY>());
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (elect_one()) tma_store_wait_all();
@@ -722,15 +858,24 @@ struct FormCost {
 };
 constexpr FormCost FORMS[] = {{64, false, 3400, 460, 251},  {128, false, 3400, 650, 270},  {192, false, 3400, 1030, 296}, {256, false, 3400, 1640, 344},
                               {128, true, 4000, 700, 228}, {192, true, 4000, 1030, 239}, {256, true, 4000, 1460, 279}};
-TileForm choose_form(const fp4_ctx* ctx, const MxGemm& g) {
-  const int64_t kbs = (g.C + 255) / 256;
+TileForm choose_form(const fp4_ctx* ctx, const MxGemm* g, int n) {
   TileForm best = {64, false, -1};
   for (const FormCost& f : FORMS) {
     const int64_t rows = f.pair ? 2 * BM : BM, workers = f.pair ? ctx->num_sms / 2 : ctx->num_sms;
     if (!workers) continue;
-    const int64_t rounds = ((g.I + rows - 1) / rows * ((g.J + f.bn - 1) / f.bn) + workers - 1) / workers;
-    const int64_t cost = f.launch + rounds * (f.tile + kbs * f.k_block * (g.format == FP4_MX_NVFP4 ? 11 : 10) / 10);
-    if (best.cost < 0 || cost < best.cost) best = {f.bn, f.pair, cost};
+    int64_t tiles[2] = {0, 0}, each[2] = {0, 0};
+    for (int i = 0; i < n; ++i) {
+      tiles[i] = (g[i].I + rows - 1) / rows * ((g[i].J + f.bn - 1) / f.bn);
+      each[i] = f.tile + (g[i].C + 255) / 256 * f.k_block * (g[i].format == FP4_MX_NVFP4 ? 11 : 10) / 10;
+    }
+    // worker r takes tiles r, r + workers, ...: the busiest is the first one, or the first one that begins with the second product
+    int64_t busiest = 0;
+    for (const int64_t r : {int64_t(0), tiles[0] % workers}) {
+      const int64_t first = (tiles[0] - r + workers - 1) / workers, all = (tiles[0] + tiles[1] - r + workers - 1) / workers;
+      const int64_t t = first * each[0] + (all - first) * each[1];
+      if (t > busiest) busiest = t;
+    }
+    if (best.cost < 0 || f.launch + busiest < best.cost) best = {f.bn, f.pair, f.launch + busiest};
   }
   return best;
 }
@@ -751,51 +896,58 @@ FewForm choose_few(const fp4_ctx* ctx, const MxGemm& g) {
   return {int(splits), 4100 + (splits > 1 ? 300 : 0) + rounds * one};
 }
 
-template <int FMT, bool PAIR, int DT>
-int launch_tiles_as(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int32_t* status) {
+template <int FMT, bool PAIR, int DT, bool ALIGNED>
+int launch_tiles_as(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, int bn, int32_t* status) {
   constexpr int CTAS = PAIR ? 2 : 1;
-  CUtensorMap a, b, sa, sb, out = {};
   GemmArgs args = {};
-  args.num_k_blocks = int((g.C + 255) / 256);
-  args.num_m_blocks = int((g.I + CTAS * BM - 1) / (CTAS * BM));
   args.bn = bn;
-  args.num_n_blocks = int((g.J + bn - 1) / bn);
   args.b_tiles = (bn + 127) / 128;
   args.stage_bytes = A_BYTES + bn * 128 / CTAS + scale_bytes(FMT) * (1 + args.b_tiles);
   args.tx_bytes = uint32_t(args.stage_bytes);
   args.stages = (MOST_SMEM - FIXED_SMEM) / args.stage_bytes;
   if (args.stages > MAX_STAGES) args.stages = MAX_STAGES;
   args.idesc = idesc_mx(FMT, CTAS * BM, bn);
-  args.out = out_args(g);
-  args.powers = powers_of(g);
   args.status = status;
   args.wait_limit_ns = wait_limit(ctx);
-  int rc = make_codes_map(ctx, &a, g.a, g.I, g.C, BM);
-  if (rc == FP4_OK) rc = make_codes_map(ctx, &b, g.b, g.J, g.C, bn / CTAS);
-  if (rc == FP4_OK) rc = make_scales_map(ctx, &sa, g.a_scales, g.I, g.C, FMT, 1);
-  if (rc == FP4_OK) rc = make_scales_map(ctx, &sb, g.b_scales, g.J, g.C, FMT, args.b_tiles);
-  if (rc == FP4_OK && args.out.bulk) {
-    const CUtensorMapDataType type = g.dtype == FP4_DTYPE_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                     : g.dtype == FP4_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                                 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    const uint32_t elt = g.dtype == FP4_DTYPE_FP32 ? 4 : 2;
-    rc = make_map(ctx, &out, type, g.out, uint64_t(g.J), uint64_t(g.I), uint64_t(g.ld) * elt, 64 / elt, 32, CU_TENSOR_MAP_SWIZZLE_64B,
-                  CU_TENSOR_MAP_L2_PROMOTION_NONE);
+  int64_t tiles = 0;
+  for (int i = 0; i < n; ++i) {
+    Problem& p = args.p[i];
+    const MxGemm& q = g[i];
+    p.num_k_blocks = int((q.C + 255) / 256);
+    p.num_m_blocks = int((q.I + CTAS * BM - 1) / (CTAS * BM));
+    p.num_n_blocks = int((q.J + bn - 1) / bn);
+    tiles += int64_t(p.num_m_blocks) * p.num_n_blocks;
+    p.to = out_args(q);
+    p.powers = powers_of(q);
+    int rc = make_codes_map(ctx, &p.a, q.a, q.I, q.C, BM);
+    if (rc == FP4_OK) rc = make_codes_map(ctx, &p.b, q.b, q.J, q.C, bn / CTAS);
+    if (rc == FP4_OK) rc = make_scales_map(ctx, &p.sa, q.a_scales, q.I, q.C, FMT, 1);
+    if (rc == FP4_OK) rc = make_scales_map(ctx, &p.sb, q.b_scales, q.J, q.C, FMT, args.b_tiles);
+    if (rc == FP4_OK && ALIGNED) {
+      const CUtensorMapDataType type = DT == FP4_DTYPE_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                       : DT == FP4_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                              : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+      constexpr uint32_t elt = DT == FP4_DTYPE_FP32 ? 4 : 2;
+      rc = make_map(ctx, &p.out, type, q.out, uint64_t(q.J), uint64_t(q.I), uint64_t(q.ld) * elt, 64 / elt, 32, CU_TENSOR_MAP_SWIZZLE_64B,
+                    CU_TENSOR_MAP_L2_PROMOTION_NONE);
+    }
+    if (rc != FP4_OK) return rc;
   }
-  if (rc != FP4_OK) return rc;
-  constexpr auto kernel = mx_gemm_kernel<FMT, PAIR, DT>;
+  constexpr auto kernel = mx_gemm_kernel<FMT, PAIR, DT, ALIGNED>;
   FP4_CUDA_TRY(mx_allow_smem<kernel>(ctx->device, MOST_SMEM));
-  const int64_t tiles = int64_t(args.num_m_blocks) * args.num_n_blocks, most = ctx->num_sms / CTAS;
+  const int64_t most = ctx->num_sms / CTAS;
   KernelScope scope(ctx, stream, KC_GEMM, 1);
-  return mx_launch<kernel>(dim3(unsigned(CTAS * (tiles < most ? tiles : most))), THREADS, FIXED_SMEM + args.stages * args.stage_bytes, CTAS, stream, a, b,
-                           sa, sb, out, args);
+  return mx_launch<kernel>(dim3(unsigned(CTAS * (tiles < most ? tiles : most))), THREADS, FIXED_SMEM + args.stages * args.stage_bytes, CTAS, stream, args);
 }
-
-template <int FMT, bool PAIR>
-int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int bn, int32_t* status) {
-  if (g.dtype == FP4_DTYPE_BF16) return launch_tiles_as<FMT, PAIR, FP4_DTYPE_BF16>(ctx, stream, g, bn, status);
-  if (g.dtype == FP4_DTYPE_FP16) return launch_tiles_as<FMT, PAIR, FP4_DTYPE_FP16>(ctx, stream, g, bn, status);
-  return launch_tiles_as<FMT, PAIR, FP4_DTYPE_FP32>(ctx, stream, g, bn, status);
+template <int FMT>
+int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, const TileForm& f, int32_t* status) {
+  const bool aligned = out_args(g[0]).bulk && (n == 1 || out_args(g[1]).bulk);
+#define AS(PAIR, DT) \
+  (aligned ? launch_tiles_as<FMT, PAIR, DT, true>(ctx, stream, g, n, f.bn, status) : launch_tiles_as<FMT, PAIR, DT, false>(ctx, stream, g, n, f.bn, status))
+  if (g->dtype == FP4_DTYPE_BF16) return f.pair ? AS(true, FP4_DTYPE_BF16) : AS(false, FP4_DTYPE_BF16);
+  if (g->dtype == FP4_DTYPE_FP16) return f.pair ? AS(true, FP4_DTYPE_FP16) : AS(false, FP4_DTYPE_FP16);
+  return f.pair ? AS(true, FP4_DTYPE_FP32) : AS(false, FP4_DTYPE_FP32);
+#undef AS
 }
 
 template <int FMT>
@@ -838,13 +990,25 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, i
 
 }  // namespace
 
-int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int32_t* status) {
-  const bool nv = g.format == FP4_MX_NVFP4;
-  const TileForm f = choose_form(ctx, g);
-  if (g.I <= FEW_ROWS) {
-    const FewForm few = choose_few(ctx, g);
-    if (few.cost <= f.cost) return nv ? launch_few<FP4_MX_NVFP4>(ctx, stream, g, few.splits, status) : launch_few<FP4_MX_E2M1>(ctx, stream, g, few.splits, status);
+int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, int32_t* status) {
+  const bool nv = g->format == FP4_MX_NVFP4;
+  // Two products in one launch: of one type, and neither with so few rows that it has a kernel of its own.  The one whose tiles take longer
+  // comes first.
+  if (n == 2) {
+    bool apart = g[0].dtype != g[1].dtype;
+    for (int i = 0; i < 2; ++i) apart = apart || (g[i].I <= FEW_ROWS && choose_few(ctx, g[i]).cost <= choose_form(ctx, g + i, 1).cost);
+    if (apart) {
+      const int rc = launch_mx_gemm(ctx, stream, g, 1, status);
+      return rc != FP4_OK ? rc : launch_mx_gemm(ctx, stream, g + 1, 1, status);
+    }
+    const MxGemm in_order[2] = {g[g[1].C > g[0].C], g[g[1].C <= g[0].C]};
+    const TileForm o = choose_form(ctx, in_order, 2);
+    return nv ? launch_tiles<FP4_MX_NVFP4>(ctx, stream, in_order, 2, o, status) : launch_tiles<FP4_MX_E2M1>(ctx, stream, in_order, 2, o, status);
   }
-  if (f.pair) return nv ? launch_tiles<FP4_MX_NVFP4, true>(ctx, stream, g, f.bn, status) : launch_tiles<FP4_MX_E2M1, true>(ctx, stream, g, f.bn, status);
-  return nv ? launch_tiles<FP4_MX_NVFP4, false>(ctx, stream, g, f.bn, status) : launch_tiles<FP4_MX_E2M1, false>(ctx, stream, g, f.bn, status);
+  const TileForm f = choose_form(ctx, g, 1);
+  if (g->I <= FEW_ROWS) {
+    const FewForm few = choose_few(ctx, *g);
+    if (few.cost <= f.cost) return nv ? launch_few<FP4_MX_NVFP4>(ctx, stream, *g, few.splits, status) : launch_few<FP4_MX_E2M1>(ctx, stream, *g, few.splits, status);
+  }
+  return nv ? launch_tiles<FP4_MX_NVFP4>(ctx, stream, g, 1, f, status) : launch_tiles<FP4_MX_E2M1>(ctx, stream, g, 1, f, status);
 }

@@ -483,9 +483,9 @@ __device__ __forceinline__ void copy_scales(uint8_t* dst, const uint8_t* smem, i
 struct TileAt {
   int64_t row, col;            // tile coordinates
 };
-__device__ __forceinline__ TileAt tile_at(int64_t col_tiles) {
-  const int64_t t = blockIdx.x;
-  return {t / col_tiles, t % col_tiles};
+__device__ __forceinline__ TileAt tile_at(unsigned t, int64_t col_tiles) {
+  const unsigned per_row = unsigned(col_tiles);
+  return {int64_t(t / per_row), int64_t(t % per_row)};
 }
 __device__ __forceinline__ void report(bool bad, int32_t* status) {
   if (__any_sync(0xFFFFFFFFu, bad) && (threadIdx.x & 31) == 0) atomicOr(status, FP4_DEV_NONFINITE);
@@ -558,24 +558,31 @@ __device__ __forceinline__ uint32_t amax_of(const AmaxArgs& a, int64_t warp, int
   else m &= 0x7FFFFFFFu;
   return block_max(__float_as_uint(TypeOf<T>::value(m)), s_max);
 }
+// One matrix or two in a launch: the first has the first `blocks` blocks.
+struct AmaxBatch {
+  AmaxArgs a[2];
+  int blocks[2];
+};
 template <class T>
-__global__ void __launch_bounds__(THREADS) mx_amax_kernel(const __grid_constant__ AmaxArgs a) {
+__global__ void __launch_bounds__(THREADS) mx_amax_kernel(const __grid_constant__ AmaxBatch batch) {
   __shared__ uint32_t s_max[THREADS / 32];
+  const int second = int(blockIdx.x) >= batch.blocks[0], block = int(blockIdx.x) - (second ? batch.blocks[0] : 0), blocks = batch.blocks[second];
+  const AmaxArgs& a = batch.a[second];
   mx_wait_for_inputs();
   mx_let_next_start();
-  const uint32_t m = amax_of<T>(a, int64_t(blockIdx.x) * (THREADS / 32) + (threadIdx.x >> 5), int64_t(gridDim.x) * (THREADS / 32), s_max);
-  if (threadIdx.x == 0) a.parts[blockIdx.x] = m;
+  const uint32_t m = amax_of<T>(a, int64_t(block) * (THREADS / 32) + (threadIdx.x >> 5), int64_t(blocks) * (THREADS / 32), s_max);
+  if (threadIdx.x == 0) a.parts[block] = m;
   if (!a.amax) return;
   __shared__ bool last;
   if (threadIdx.x == 0) {
     __threadfence();
-    last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    last = atomicAdd(a.ticket, 1u) == unsigned(blocks) - 1;
     __threadfence();
   }
   __syncthreads();
   if (!last) return;
   uint32_t all = 0;
-  for (unsigned i = threadIdx.x; i < gridDim.x; i += THREADS) all = max(all, *const_cast<volatile uint32_t*>(a.parts + i));
+  for (int i = threadIdx.x; i < blocks; i += THREADS) all = max(all, *const_cast<volatile uint32_t*>(a.parts + i));
   all = block_max(all, s_max);
   if (threadIdx.x == 0) {
     *a.amax = all;
@@ -593,10 +600,16 @@ struct QuantArgs {
   uint32_t* amax;
   const uint32_t* part;
   int parts;
+  bool backwards;              // the last tile first: what the pass for the amax has left in L2
   int32_t* status;
 };
+// One tensor or two in a launch.
+struct QuantBatch {
+  QuantArgs a[2];
+  unsigned tiles[2];
+};
 template <class T, int FMT, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_constant__ QuantArgs a) {
+__global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_constant__ QuantBatch batch) {
   constexpr int CODE_BYTES = MX_TILE * code_row_bytes(FMT);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tile = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -604,7 +617,10 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
   uint8_t* s_across = s_along + (ROWS ? CODE_BYTES : 0);
   __shared__ __align__(16) uint8_t s_scale[2][1024];
   __shared__ Loader l;
-  const TileAt at = tile_at(mx_tiles(a.cols));
+  const int second = blockIdx.x >= batch.tiles[0];
+  const QuantArgs& a = batch.a[second];
+  const unsigned t = blockIdx.x - (second ? batch.tiles[0] : 0u);
+  const TileAt at = tile_at(a.backwards ? batch.tiles[second] - 1 - t : t, mx_tiles(a.cols));
   const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
   if (threadIdx.x == 0) {
     mbar_init(&l.bar, 1);
@@ -635,7 +651,7 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
     } else {
       m = *a.amax;
     }
-    if (a.parts && blockIdx.x == 0 && threadIdx.x == 0) *a.amax = m;
+    if (a.parts && t == 0 && threadIdx.x == 0) *a.amax = m;
     const int k = mx_tensor_exponent(m);
     tensor = make_float2(pow2_int(k), pow2_int(-k));
   }
@@ -707,7 +723,7 @@ __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_con
   __shared__ __align__(16) uint8_t s_scale[BYTES];
   __shared__ Loader l;
   const int64_t col_tiles = mx_tiles(a.cols);
-  const TileAt at = tile_at(col_tiles);
+  const TileAt at = tile_at(blockIdx.x, col_tiles);
   const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
   if (threadIdx.x == 0) {
     mbar_init(&l.bar, 1);
@@ -807,7 +823,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd
   uint8_t* s_across = s_along + (a.along.on ? CODES4 : 0);
   __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
   __shared__ Loader l;
-  const TileAt at = tile_at(mx_tiles(a.cols));
+  const TileAt at = tile_at(blockIdx.x, mx_tiles(a.cols));
   const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
   if (threadIdx.x == 0) {
     mbar_init(&l.bar, 1);
@@ -878,7 +894,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_sw
   uint8_t* s_across = s_along + (H && a.along.on ? CODES4 : 0);
   __shared__ __align__(16) uint8_t s_scale[4][512];        // along, across, gate, up
   __shared__ Loader l;
-  const TileAt at = tile_at(mx_tiles(a.cols));
+  const TileAt at = tile_at(blockIdx.x, mx_tiles(a.cols));
   const int64_t row0 = at.row * MX_TILE, col0 = at.col * MX_TILE;
   if (threadIdx.x == 0) {
     mbar_init(&l.bar, 1);
@@ -1001,52 +1017,71 @@ int codes_across(fp4_ctx* ctx, Codes* c, const fp4_mx_tensor& q, int64_t rows, i
   return c->on ? codes_side(ctx, &c->codes, q.codes_t, cols, rows, q.format) : FP4_OK;
 }
 template <auto KERNEL, class A>
-int launch_tiles(fp4_ctx* ctx, int64_t rows, int64_t cols, int most_smem, int smem, cudaStream_t stream, const A& args) {
+int launch_tiles(fp4_ctx* ctx, int64_t tiles, int most_smem, int smem, cudaStream_t stream, const A& args) {
   FP4_CUDA_TRY(mx_allow_smem<KERNEL>(ctx->device, 1024 + most_smem));
-  return mx_launch<KERNEL>(dim3(unsigned(mx_tiles(rows) * mx_tiles(cols))), THREADS, 1024 + smem, 1, stream, args);
+  return mx_launch<KERNEL>(dim3(unsigned(tiles)), THREADS, 1024 + smem, 1, stream, args);
 }
 
 template <class T, int FMT>
-int quantize_as(fp4_ctx* ctx, cudaStream_t stream, const QuantArgs& a) {
+int quantize_as(fp4_ctx* ctx, cudaStream_t stream, const QuantBatch& q) {
   constexpr int codes = MX_TILE * code_row_bytes(FMT), one = tile_bytes<T>() + codes;
-  if (a.along.on && a.across.on) return launch_tiles<mx_quantize_kernel<T, FMT, true, true>>(ctx, a.rows, a.cols, one + codes, one + codes, stream, a);
-  if (a.across.on) return launch_tiles<mx_quantize_kernel<T, FMT, false, true>>(ctx, a.rows, a.cols, one, one, stream, a);
-  return launch_tiles<mx_quantize_kernel<T, FMT, true, false>>(ctx, a.rows, a.cols, one, one, stream, a);
+  const int64_t tiles = int64_t(q.tiles[0]) + q.tiles[1];
+  if (q.a[0].along.on && q.a[0].across.on) return launch_tiles<mx_quantize_kernel<T, FMT, true, true>>(ctx, tiles, one + codes, one + codes, stream, q);
+  if (q.a[0].across.on) return launch_tiles<mx_quantize_kernel<T, FMT, false, true>>(ctx, tiles, one, one, stream, q);
+  return launch_tiles<mx_quantize_kernel<T, FMT, true, false>>(ctx, tiles, one, one, stream, q);
 }
+// What has to be known of the tensors before they are quantised: for NVFP4 their amax.
 template <class T>
-int quantize_from(fp4_ctx* ctx, cudaStream_t stream, QuantArgs a, const fp4_mx_tensor& q) {
-  if (q.format == FP4_MX_NVFP4 && !(q.flags & FP4_MX_AMAX_GIVEN)) {
-    // Rows without a gap are one long row.
-    const bool dense = a.x.ld == a.cols;
-    AmaxArgs m = {a.x.p, dense ? 1 : a.rows, dense ? a.rows * a.cols : a.cols, a.x.ld, ctx->mx_scratch, nullptr, nullptr};
+int find_amax(fp4_ctx* ctx, cudaStream_t stream, QuantBatch& batch, const fp4_mx_tensor* const* q, int n) {
+  constexpr int MOST = MX_SCRATCH_WORDS / 2 - 1;           // parts of a tensor; the scratch ends with two tickets
+  AmaxBatch m = {};
+  int found = 0;
+  for (int i = 0; i < n; ++i) {
+    QuantArgs& a = batch.a[i];
+    if (q[i]->flags & FP4_MX_AMAX_GIVEN) continue;
     const int64_t bytes = a.rows * a.cols * int64_t(sizeof(T));
     if (bytes <= MX_SMALL_BYTES) {
       a.parts = -1;
-    } else {
-      const int64_t n = (bytes + 8 * 4096 - 1) / (8 * 4096), most = int64_t(ctx->num_sms) * 4 < MX_SCRATCH_WORDS - 1 ? int64_t(ctx->num_sms) * 4 : MX_SCRATCH_WORDS - 1;
-      const int blocks = int(n < most ? n : most);
-      if (blocks <= MX_FEW_PARTS) {
-        a.parts = blocks;
-        a.part = ctx->mx_scratch;
-      } else {
-        m.amax = a.amax;
-        m.ticket = ctx->mx_scratch + MX_SCRATCH_WORDS - 1;
-      }
-      KernelScope scope(ctx, stream, KC_ABSMAX, 1);
-      const int rc = mx_launch<mx_amax_kernel<T>>(dim3(unsigned(blocks)), THREADS, 0, 1, stream, m);
-      if (rc != FP4_OK) return rc;
+      continue;
     }
+    const int64_t want = (bytes + 8 * 4096 - 1) / (8 * 4096);
+    int blocks = ctx->num_sms * (n > 1 ? 2 : 3);
+    if (blocks > MOST) blocks = MOST;
+    if (blocks > want) blocks = int(want);
+    const bool dense = a.x.ld == a.cols;                   // rows without a gap are one long row
+    uint32_t* parts = ctx->mx_scratch + i * MOST;
+    m.a[found] = {a.x.p, dense ? 1 : a.rows, dense ? a.rows * a.cols : a.cols, a.x.ld, parts, nullptr, nullptr};
+    if (blocks <= MX_FEW_PARTS) {
+      a.parts = blocks;
+      a.part = parts;
+    } else {
+      m.a[found].amax = a.amax;
+      m.a[found].ticket = ctx->mx_scratch + MX_SCRATCH_WORDS - 1 - i;
+    }
+    a.backwards = true;
+    m.blocks[found++] = blocks;
+  }
+  if (!found) return FP4_OK;
+  KernelScope scope(ctx, stream, KC_ABSMAX, 1);
+  return mx_launch<mx_amax_kernel<T>>(dim3(unsigned(m.blocks[0] + m.blocks[1])), THREADS, 0, 1, stream, m);
+}
+template <class T>
+int quantize_from(fp4_ctx* ctx, cudaStream_t stream, QuantBatch& batch, const fp4_mx_tensor* const* q, int n) {
+  const int format = q[0]->format;
+  if (format == FP4_MX_NVFP4) {
+    const int rc = find_amax<T>(ctx, stream, batch, q, n);
+    if (rc != FP4_OK) return rc;
   }
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
-  if (q.format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(ctx, stream, a);
-  if (q.format == FP4_MX_NVFP4) return quantize_as<T, FP4_MX_NVFP4>(ctx, stream, a);
-  return quantize_as<T, FP4_MX_E4M3>(ctx, stream, a);
+  if (format == FP4_MX_E2M1) return quantize_as<T, FP4_MX_E2M1>(ctx, stream, batch);
+  if (format == FP4_MX_NVFP4) return quantize_as<T, FP4_MX_NVFP4>(ctx, stream, batch);
+  return quantize_as<T, FP4_MX_E4M3>(ctx, stream, batch);
 }
 
 template <class T, int FMT>
 int dequantize_as(fp4_ctx* ctx, cudaStream_t stream, const DequantArgs& a) {
   constexpr int smem = tile_bytes<T>() + MX_TILE * code_row_bytes(FMT);
-  return launch_tiles<mx_dequantize_kernel<T, FMT>>(ctx, a.rows, a.cols, smem, smem, stream, a);
+  return launch_tiles<mx_dequantize_kernel<T, FMT>>(ctx, mx_tiles(a.rows) * mx_tiles(a.cols), smem, smem, stream, a);
 }
 template <class T>
 int dequantize_to(fp4_ctx* ctx, cudaStream_t stream, const DequantArgs& a, int format) {
@@ -1060,10 +1095,10 @@ int swiglu_as(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, bool bwd) 
   constexpr int codes4 = MX_TILE * 64, tile = tile_bytes<T>();
   const int more = (a.along.on ? codes4 : 0) + (a.across.on ? codes4 : 0);
   if (bwd && (a.has_h || more))
-    return launch_tiles<mx_swiglu_bwd_kernel<T, true>>(ctx, a.rows, a.cols, 3 * tile + 2 * codes4, 3 * tile + more, stream, a);
-  if (bwd) return launch_tiles<mx_swiglu_bwd_kernel<T, false>>(ctx, a.rows, a.cols, 2 * tile, 2 * tile, stream, a);
-  if (a.ckpt_gate.on) return launch_tiles<mx_swiglu_fwd_kernel<T, true>>(ctx, a.rows, a.cols, 2 * tile + 2 * codes4, 2 * tile + more, stream, a);
-  return launch_tiles<mx_swiglu_fwd_kernel<T, false>>(ctx, a.rows, a.cols, 2 * tile + 2 * codes4, 2 * tile + more, stream, a);
+    return launch_tiles<mx_swiglu_bwd_kernel<T, true>>(ctx, mx_tiles(a.rows) * mx_tiles(a.cols), 3 * tile + 2 * codes4, 3 * tile + more, stream, a);
+  if (bwd) return launch_tiles<mx_swiglu_bwd_kernel<T, false>>(ctx, mx_tiles(a.rows) * mx_tiles(a.cols), 2 * tile, 2 * tile, stream, a);
+  if (a.ckpt_gate.on) return launch_tiles<mx_swiglu_fwd_kernel<T, true>>(ctx, mx_tiles(a.rows) * mx_tiles(a.cols), 2 * tile + 2 * codes4, 2 * tile + more, stream, a);
+  return launch_tiles<mx_swiglu_fwd_kernel<T, false>>(ctx, mx_tiles(a.rows) * mx_tiles(a.cols), 2 * tile + 2 * codes4, 2 * tile + more, stream, a);
 }
 int swiglu(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, int dtype, bool bwd) {
   KernelScope scope(ctx, stream, KC_ENCODE, 1);
@@ -1074,19 +1109,34 @@ int swiglu(fp4_ctx* ctx, cudaStream_t stream, const SwigluArgs& a, int dtype, bo
 
 }  // namespace
 
-int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, MxMatrix x, int dtype, const fp4_mx_tensor& q, int32_t* status) {
-  QuantArgs a = {};
-  a.rows = q.rows;
-  a.cols = q.cols;
-  a.amax = reinterpret_cast<uint32_t*>(q.amax);
-  a.status = status;
-  int rc = matrix_side(ctx, &a.x, x, q.rows, q.cols, dtype, false);
-  if (rc == FP4_OK) rc = codes_along(ctx, &a.along, q, q.rows, q.cols);
-  if (rc == FP4_OK) rc = codes_across(ctx, &a.across, q, q.rows, q.cols);
-  if (rc != FP4_OK) return rc;
-  if (dtype == FP4_DTYPE_BF16) return quantize_from<__nv_bfloat16>(ctx, stream, a, q);
-  if (dtype == FP4_DTYPE_FP16) return quantize_from<__half>(ctx, stream, a, q);
-  return quantize_from<float>(ctx, stream, a, q);
+int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize* what, int n, int32_t* status) {
+  const int dtype = what[0].dtype;
+  if (n == 2) {                                            // one launch takes two of a kind
+    const fp4_mx_tensor &p = *what[0].q, &q = *what[1].q;
+    if (what[1].dtype != dtype || p.format != q.format || !p.codes != !q.codes || !p.codes_t != !q.codes_t ||
+        mx_tiles(p.rows) * mx_tiles(p.cols) + mx_tiles(q.rows) * mx_tiles(q.cols) > 0x7FFFFFFF) {
+      const int rc = launch_mx_quantize(ctx, stream, what, 1, status);
+      return rc != FP4_OK ? rc : launch_mx_quantize(ctx, stream, what + 1, 1, status);
+    }
+  }
+  QuantBatch batch = {};
+  const fp4_mx_tensor* q[2] = {};
+  for (int i = 0; i < n; ++i) {
+    QuantArgs& a = batch.a[i];
+    q[i] = what[i].q;
+    a.rows = q[i]->rows;
+    a.cols = q[i]->cols;
+    a.amax = reinterpret_cast<uint32_t*>(q[i]->amax);
+    a.status = status;
+    batch.tiles[i] = unsigned(mx_tiles(a.rows) * mx_tiles(a.cols));
+    int rc = matrix_side(ctx, &a.x, what[i].x, a.rows, a.cols, dtype, false);
+    if (rc == FP4_OK) rc = codes_along(ctx, &a.along, *q[i], a.rows, a.cols);
+    if (rc == FP4_OK) rc = codes_across(ctx, &a.across, *q[i], a.rows, a.cols);
+    if (rc != FP4_OK) return rc;
+  }
+  if (dtype == FP4_DTYPE_BF16) return quantize_from<__nv_bfloat16>(ctx, stream, batch, q, n);
+  if (dtype == FP4_DTYPE_FP16) return quantize_from<__half>(ctx, stream, batch, q, n);
+  return quantize_from<float>(ctx, stream, batch, q, n);
 }
 
 int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes, const uint8_t* scales, const float* amax,
