@@ -880,8 +880,8 @@ TileForm choose_form(const fp4_ctx* ctx, const MxGemm* g, int n) {
   return best;
 }
 
-// Few rows: into how many parts a cluster splits the contraction, and the time by the same kind of model.  More than four parts, or more CTAs
-// than SMs, cost more than they save (clusters of 8 do not fill the GPU: 1 x 4096 x 4096 5.0 us in 4 parts, 7.3 in 8; not split 6.8).
+// Few rows: into how many parts a cluster splits the contraction, and the time by the same kind of model.  As a rule more than four parts, or
+// more CTAs than SMs, cost more than they save (clusters of 8 do not fill the GPU: 1 x 4096 x 4096 5.0 us in 4 parts, 7.3 in 8; not split 6.8).
 struct FewForm {
   int splits;
   int64_t cost;
@@ -891,6 +891,11 @@ FewForm choose_few(const fp4_ctx* ctx, const MxGemm& g) {
   int64_t splits = ctx->num_sms / tiles;
   if (splits > (kbs + 1) / 2) splits = (kbs + 1) / 2;
   splits = splits < 1 ? 1 : (splits > 4 ? 4 : splits);
+  // (two CTAs an SM, where each still has a long way to go and the tokens take little room: 24 x 5120 x 13824 in blocks of 16, 6 parts 8.8 us, 3 parts 9.6)
+  int64_t more = 2 * ctx->num_sms / tiles;
+  if (more > kbs / 8) more = kbs / 8;
+  if (more > 6) more = 6;
+  if (g.I <= 32 && more > splits) splits = more;
   const int64_t rounds = (tiles + 2 * ctx->num_sms - 1) / (2 * ctx->num_sms);
   const int64_t one = (kbs + splits - 1) / splits * (g.format == FP4_MX_NVFP4 ? 200 : 150) + 15 * ((g.I + 15) / 16 * 16);
   return {int(splits), 4100 + (splits > 1 ? 300 : 0) + rounds * one};
@@ -960,7 +965,7 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, i
   args.splits = splits;
   args.stage_bytes = A_BYTES + args.nt * 128 + 2 * scale_bytes(FMT);
   // (more CTAs than SMs: two on each)
-  args.stages = ((tiles > ctx->num_sms ? 113 * 1024 : MOST_SMEM) - 1024 - MISC_BYTES) / args.stage_bytes;
+  args.stages = ((tiles * splits > ctx->num_sms ? 113 * 1024 : MOST_SMEM) - 1024 - MISC_BYTES) / args.stage_bytes;
   if (args.stages > FEW_MAX_STAGES) args.stages = FEW_MAX_STAGES;
   const int per_cta = (args.num_k_blocks + args.splits - 1) / args.splits;
   if (args.stages > per_cta) args.stages = per_cta;

@@ -22,6 +22,8 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "mx.cuh"
 #include "tc_ptx.cuh"
 
@@ -376,66 +378,163 @@ __device__ __forceinline__ void request_tile(const Side& s, Loader* l, uint8_t* 
 #pragma unroll
   for (int i = 0; i < tile_bytes<T>() / BOX_BYTES; ++i) tma_load_2d(tile + i * BOX_BYTES, &s.map, &l->bar, int(col0) + i * PER, int(row0));
 }
-// Rows off 16-byte boundaries, in: a lane takes 16 bytes of the tile's row, from the two aligned pieces that hold them, shifted into
+// Rows off 16-byte boundaries.  A tile that lies whole in the matrix goes without checks, but for its first and last 16 bytes, whose aligned
+// pieces may hold bytes that are not the matrix's.  Rows 16 / sizeof(T) apart lie alike within 16 bytes, so a warp takes such
+// rows together: how far its pieces are to be shifted is the same in all lanes.
+template <class T>
+__device__ __forceinline__ bool whole_tile(const Side& s, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+  return col0 + MX_TILE <= cols && row0 + MX_TILE <= rows;
+}
+// Words first .. first + 4 of eight, shifted right by `bits`, to `put`.
+template <int E, class Put>
+__device__ __forceinline__ void shifted(const uint4& lo, const uint4& hi, int mis, Put put) {
+  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  const int bits = (mis & 3) * 8;
+  const auto from = [&](auto first) {
+    constexpr int F = decltype(first)::value;
+    uint32_t x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = E == 4 ? w[F + k] : __funnelshift_r(w[F + k], w[F + k + 1], bits);
+    put(make_uint4(x[0], x[1], x[2], x[3]));
+  };
+  switch (mis >> 2) {
+    case 0: from(std::integral_constant<int, 0>()); break;
+    case 1: from(std::integral_constant<int, 1>()); break;
+    case 2: from(std::integral_constant<int, 2>()); break;
+    default: from(std::integral_constant<int, 3>()); break;
+  }
+}
+// The warp's rows: step i takes row first_row + i (and, of 16 bits, the row eight further in the upper half of the lanes).
+template <class T>
+struct WarpRows {
+  static constexpr int E = int(sizeof(T)), UNITS = MX_TILE * E / 16, STEPS = MX_TILE / 8 / (32 / UNITS);
+  int row, unit;
+  __device__ __forceinline__ WarpRows() {
+    const int lane = threadIdx.x & 31;
+    row = int(threadIdx.x >> 5) * 16 + lane / UNITS * 8;
+    unit = lane % UNITS;
+  }
+};
+// Eight 32-bit words of a lane: two aligned pieces, or elements one by one.
+struct Words8 {
+  uint4 lo, hi;
+};
+template <class T>
+__device__ __forceinline__ Words8 load_elements(const void* p, int n) {       // the first n of 16 / sizeof(T)
+  uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 16 / int(sizeof(T)); ++i)
+    if (i < n) w[i] = sizeof(T) == 4 ? static_cast<const uint32_t*>(p)[i] : static_cast<const unsigned short*>(p)[i];
+  return {make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])};
+}
+template <class T>
+__device__ __forceinline__ uint4 join_elements(const Words8& v) {
+  if constexpr (sizeof(T) == 4) return v.lo;
+  else return make_uint4(v.lo.x | v.lo.y << 16, v.lo.z | v.lo.w << 16, v.hi.x | v.hi.y << 16, v.hi.z | v.hi.w << 16);
+}
+template <class T>
+__device__ __forceinline__ void copy_whole_tile_in(const Side& s, uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+  constexpr int E = int(sizeof(T)), AT_ONCE = 4;
+  const WarpRows<T> at;
+  // (only the matrix's first 16 bytes and its last ones can lie in pieces that reach beyond it: rows of a whole tile are long enough)
+  const uint8_t *first = static_cast<const uint8_t*>(s.p), *last = first + ((rows - 1) * s.ld + cols) * E;
+  const bool at_end = row0 == 0 || row0 + MX_TILE == rows;
+  const uint8_t* p = static_cast<const uint8_t*>(s.p) + ((row0 + at.row) * s.ld + col0) * E + at.unit * 16;
+  const int64_t pitch = s.ld * E;
+#pragma unroll 1
+  for (int i0 = 0; i0 < WarpRows<T>::STEPS; i0 += AT_ONCE) {
+    Words8 v[AT_ONCE];
+    int mis[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      mis[j] = int(reinterpret_cast<uintptr_t>(p) & 15);
+      const uint8_t* q = p - mis[j];
+      if (at_end && (q < first || q + 32 > last)) {
+        v[j] = load_elements<T>(p, 16 / E);
+        mis[j] = -1;
+      } else {
+        v[j] = {reinterpret_cast<const uint4*>(q)[0], reinterpret_cast<const uint4*>(q)[1]};
+      }
+      p += pitch;
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      uint4* to = reinterpret_cast<uint4*>(tile + at128(at.row + i0 + j, at.unit * 16));
+      if (mis[j] < 0) *to = join_elements<T>(v[j]);
+      else shifted<E>(v[j].lo, v[j].hi, mis[j], [&](const uint4& x) { *to = x; });
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ void copy_whole_tile_out(const Side& s, const uint8_t* tile, int64_t row0, int64_t col0) {
+  constexpr int E = int(sizeof(T)), PER = 16 / E, UNITS = WarpRows<T>::UNITS;
+  const WarpRows<T> at;
+  const int64_t pitch = s.ld * E;
+  uint8_t* p = static_cast<uint8_t*>(s.p) + ((row0 + at.row) * s.ld + col0) * E;
+#pragma unroll 2
+  for (int i = 0; i < WarpRows<T>::STEPS; ++i) {
+    // the piece that begins `head` bytes behind its 16 bytes' place in the tile (the last one: what is left at the ends, below)
+    const int head = int(-reinterpret_cast<intptr_t>(p) & 15), r = at.row + i;
+    if (head == 0 || at.unit < UNITS - 1) {
+      const uint4 lo = *reinterpret_cast<const uint4*>(tile + at128(r, at.unit * 16));
+      const uint4 hi = *reinterpret_cast<const uint4*>(tile + at128(r, head ? at.unit * 16 + 16 : at.unit * 16));
+      shifted<E>(lo, hi, head, [&](const uint4& v) { *reinterpret_cast<uint4*>(p + head + at.unit * 16) = v; });
+    }
+    p += pitch;
+  }
+  // PER elements of a row that begins off a boundary: those ahead of its first piece and behind its last
+  const int lane = threadIdx.x & 31, e = lane % PER * E, r0 = int(threadIdx.x >> 5) * 16 + lane / PER;
+  p = static_cast<uint8_t*>(s.p) + ((row0 + r0) * s.ld + col0) * E;
+#pragma unroll 2
+  for (int i = 0; i < 16; i += 32 / PER) {
+    const int head = int(-reinterpret_cast<intptr_t>(p) & 15), at_byte = e < head ? e : MX_TILE * E - 16 + e;
+    if (head) *reinterpret_cast<T*>(p + at_byte) = *reinterpret_cast<const T*>(tile + at128(r0 + i, at_byte));
+    p += pitch * (32 / PER);
+  }
+}
+// Any tile, in: a lane takes 16 bytes of the tile's row, from the two aligned pieces that hold them, shifted into
 // place; what would touch bytes outside of the matrix, and the row's last piece, goes element by element.
 template <class T>
 __device__ __forceinline__ void copy_tile_in(const Side& s, uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+  if (whole_tile<T>(s, row0, col0, rows, cols)) return copy_whole_tile_in<T>(s, tile, row0, col0, rows, cols);
   constexpr int E = int(sizeof(T)), PER = 16 / E, UNITS = MX_TILE / PER, STEPS = MX_TILE * UNITS / THREADS, AT_ONCE = 4;
   const uintptr_t first = reinterpret_cast<uintptr_t>(s.p), last = first + uintptr_t(((rows - 1) * s.ld + cols) * E);
   const int unit = threadIdx.x % UNITS;
   const int64_t col = col0 + unit * PER;
 #pragma unroll 1
   for (int i0 = 0; i0 < STEPS; i0 += AT_ONCE) {
-    uint4 lo[AT_ONCE], hi[AT_ONCE];
+    Words8 v[AT_ONCE];
     int how[AT_ONCE];                                      // shift in bytes; -1: element by element
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) {
       const int64_t row = row0 + (i0 + j) * (THREADS / UNITS) + threadIdx.x / UNITS;
-      lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
+      v[j] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
       how[j] = 0;
       if (row < rows && col < cols) {
         const uintptr_t at = first + uintptr_t((row * s.ld + col) * E), piece = at & ~uintptr_t(15);
         how[j] = int(at - piece);
         if (col + PER > cols || piece < first || piece + (how[j] ? 32 : 16) > last) {
           how[j] = -1;
+          v[j] = load_elements<T>(reinterpret_cast<const void*>(at), int(cols - col));
         } else {
-          lo[j] = *reinterpret_cast<const uint4*>(piece);
-          if (how[j]) hi[j] = *reinterpret_cast<const uint4*>(piece + 16);
+          v[j].lo = *reinterpret_cast<const uint4*>(piece);
+          if (how[j]) v[j].hi = *reinterpret_cast<const uint4*>(piece + 16);
         }
       }
     }
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) {
       const int r = (i0 + j) * (THREADS / UNITS) + threadIdx.x / UNITS;
-      uint32_t w[8] = {lo[j].x, lo[j].y, lo[j].z, lo[j].w, hi[j].x, hi[j].y, hi[j].z, hi[j].w};
-      if (how[j] < 0) {
-        const T* p = static_cast<const T*>(s.p) + (row0 + r) * s.ld + col;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          uint32_t bits = 0;
-          if (col + i < cols) bits = E == 4 ? *reinterpret_cast<const uint32_t*>(p + i) : *reinterpret_cast<const unsigned short*>(p + i);
-          if (E == 4) w[i] = bits;
-          else w[i / 2] = i % 2 ? w[i / 2] | (bits << 16) : bits;
-        }
-        how[j] = 0;
-      }
-      const bool two = how[j] & 8, one = how[j] & 4;
-#pragma unroll
-      for (int i = 0; i < 6; ++i) w[i] = two ? w[i + 2] : w[i];
-#pragma unroll
-      for (int i = 0; i < 5; ++i) w[i] = one ? w[i + 1] : w[i];
-      if (E == 2) {
-        const int bits = (how[j] & 3) * 8;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], bits);
-      }
-      *reinterpret_cast<uint4*>(tile + at128(r, unit * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
+      uint4* to = reinterpret_cast<uint4*>(tile + at128(r, unit * 16));
+      if (how[j] < 0) *to = join_elements<T>(v[j]);
+      else shifted<E>(v[j].lo, v[j].hi, how[j], [&](const uint4& x) { *to = x; });
     }
   }
 }
 // The same, out: whole aligned pieces of 16 bytes from where in the tile's row they lie, then what is left of a row at either end.
 template <class T>
 __device__ __forceinline__ void copy_tile_out(const Side& s, const uint8_t* tile, int64_t row0, int64_t col0, int64_t rows, int64_t cols) {
+  if (whole_tile<T>(s, row0, col0, rows, cols)) return copy_whole_tile_out<T>(s, tile, row0, col0);
   constexpr int E = int(sizeof(T)), PER = 16 / E, UNITS = MX_TILE / PER, STEPS = MX_TILE * UNITS / THREADS;
   const int width = int(cols - col0 < MX_TILE ? cols - col0 : MX_TILE) * E, unit = threadIdx.x % UNITS;
 #pragma unroll 2
