@@ -559,14 +559,16 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
         const Problem& q = args.p[t >= tiles_first];
         const int shift = (t - (t >= tiles_first ? tiles_first : 0)) / q.num_m_blocks * args.bn % 128 ? 2 : 0;
         const int num_k_blocks = q.num_k_blocks;
-        // A stage is free when the tile before the last has left it.  Wide: when the last has left the columns that both stages have.
-        const int back = wide ? 1 : 2;
-        ok = n < back || mbar_wait(&acc_empty[(n - back) & 1], uint32_t((n - back) >> 1) & 1u, abort_flag, args.status, args.wait_limit_ns);
-        if (!ok) break;
-        tc_fence_after();
         for (int kb = 0; kb < num_k_blocks; ++kb) {
           ok = mbar_wait(&full_bar[stage], phase, abort_flag, args.status, args.wait_limit_ns);
           if (!ok) break;
+          if (kb == 0) {
+            // A stage is free when the tile before the last has left it.  Wide: when the last has left the columns that both stages have, which
+            // the tensor core waits for: nothing else is left to be done between that and the first MMA.
+            const int back = wide ? 1 : 2;
+            ok = n < back || mbar_wait(&acc_empty[(n - back) & 1], uint32_t((n - back) >> 1) & 1u, abort_flag, args.status, args.wait_limit_ns);
+            if (!ok) break;
+          }
           tc_fence_after();
           const uint32_t p = smem_u32(smem + stage * STAGE_BYTES);
           issue_k_block<FMT, CTAS>(p, p + A_BYTES, p + A_BYTES + b_bytes, p + A_BYTES + b_bytes + scale_bytes(FMT), args.b_tiles, d_tmem,

@@ -6,6 +6,7 @@ on the stream that is current there.
 from __future__ import annotations
 
 import ctypes as C
+from struct import Struct
 
 import torch
 
@@ -26,7 +27,13 @@ FP4_MX_ACCUMULATE_DW = 2
 FP4_REUSE_W = 1
 FP4_REUSE_X = 2
 
-_DTYPES = {torch.bfloat16: FP4_DTYPE_BF16, torch.float16: FP4_DTYPE_FP16, torch.float32: FP4_DTYPE_FP32}
+
+class _Dtypes(dict):
+    def __missing__(self, dtype):
+        raise AssertionError(f"{dtype}: a matrix is of torch.bfloat16, torch.float16 or torch.float32")
+
+
+_DTYPES = _Dtypes({torch.bfloat16: FP4_DTYPE_BF16, torch.float16: FP4_DTYPE_FP16, torch.float32: FP4_DTYPE_FP32})
 
 
 class fp4_mx_matrix(C.Structure):
@@ -42,7 +49,7 @@ class fp4_mx_tensor(C.Structure):
 def declare(lib: C.CDLL):
     """Prototypes of the fp4_mx_* functions."""
     vp, i64, i32 = C.c_void_p, C.c_int64, C.c_int
-    mat, ten = C.POINTER(fp4_mx_matrix), C.POINTER(fp4_mx_tensor)
+    mat, ten = vp, C.POINTER(fp4_mx_tensor)          # (an fp4_mx_matrix by reference, or its bytes)
     lib.fp4_mx_pitch.argtypes, lib.fp4_mx_pitch.restype = [i64, i32], i64
     lib.fp4_mx_scale_bytes.argtypes, lib.fp4_mx_scale_bytes.restype = [i64, i64, i32], i64
     lib.fp4_mx_workspace_bytes.argtypes, lib.fp4_mx_workspace_bytes.restype = [i64, i64, i64], C.c_size_t
@@ -56,17 +63,17 @@ def declare(lib: C.CDLL):
 
 
 _stream_of = torch._C._cuda_getCurrentRawStream
-_byref = C.byref
+_pack = Struct("@Pqii").pack               # the bytes of an fp4_mx_matrix: a ctypes structure takes three times as long to make
+assert Struct("@Pqii").size == C.sizeof(fp4_mx_matrix)
 
 
 def _matrix(ctx: Context, t):
     """Structure of a matrix (None: of none)."""
     if t is None:
         return None
-    stride, dtype = t.stride(), _DTYPES.get(t.dtype)
-    assert dtype is not None and len(stride) == 2 and t.get_device() == ctx.device
-    assert stride[1] == 1 or t.shape[1] <= 1
-    return _byref(fp4_mx_matrix(t.data_ptr(), stride[0], dtype, 0))
+    rows, cols = t.stride()
+    assert t.get_device() == ctx.device and (cols == 1 or t.shape[1] <= 1)
+    return _pack(t.data_ptr(), rows, _DTYPES[t.dtype], 0)
 
 
 def _new(ctx: Context, rows: int, cols: int, dtype):
@@ -89,7 +96,7 @@ class MXTensor:
         where = lambda t: None if t is None else (t.data_ptr() or 16)                         # noqa: E731
         self.struct = fp4_mx_tensor(rows, cols, where(self.codes), where(self.scales), where(self.codes_t), where(self.scales_t),
                                     _ptr(self.amax), fmt, 0)
-        self.ref = _byref(self.struct)
+        self.ref = C.byref(self.struct)
 
 
 class SwigluCheckpoint:
