@@ -375,10 +375,12 @@ int fp4_quantile_thresholds_static(void* stream, const void* x_bf16, int64_t row
  * scale NaN and codes 0, and the call raises FP4_DEV_NONFINITE; the other blocks are as specified.
  *
  * Sizes: any, zero included (nothing is launched for an empty tensor; a product over an empty contraction is
- * 0); each at most 2^31 - 1, and at most 2^31 - 1 tiles of 128 x 128 of a tensor.  A matrix of the caller's
+ * 0); each at most 2^31 - 1 (columns of a product's result 2^30 - 1), and at most 2^31 - 1 tiles of 128 x 128
+ * of a tensor (128 x 64 of a result).  A matrix of the caller's
  * (fp4_mx_matrix) is aligned to its element type and its rows may lie apart; rows that start on 16-byte
- * boundaries are faster.  An output must not overlap an input.  The calls work on the context's device
- * whichever is current, and launch no graphs; they share the workspace rule of the other calls.
+ * boundaries are faster.  An output must not overlap an input or another output.  The calls work on the
+ * context's device whichever is current, and launch no graphs.  The rule on a context's calls holds for all
+ * of them: quantising to FP4_MX_NVFP4 uses the context's counters even where it needs no workspace.
  */
 #define FP4_MX_E2M1   0
 #define FP4_MX_NVFP4  1
@@ -435,7 +437,7 @@ int fp4_mx_dequantize(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* q, int tr
 /* out[i, j] = g_a g_b sum_c a[i, c] b[j, c], fp32 sums, rounded once; with FP4_MX_ACCUMULATE the former value
  * of out is added before the rounding.  `a` is [I x C]: the tensor's rows (`codes`), or with FP4_MX_A_T its
  * columns (`codes_t`, I = a->cols, C = a->rows); `b` [J x C] likewise.  Both have the same format, one of the
- * two in E2M1.  Products of codes and scales are exact; the tensor cores add 64 of them at a time into the
+ * two in E2M1 (they may be the same tensor).  Products of codes and scales are exact; the tensor cores add 64 of them at a time into the
  * fp32 accumulator, rounding toward zero: the result is off by at most 2^-22 (C / 64 + 1) times the sum of
  * the products' magnitudes.
  * One row (a single token) up: with I <= 128 the rows of b spread over the GPU and clusters split the contraction. */
@@ -453,7 +455,8 @@ int fp4_mx_gemm(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* a, const fp4_mx
  * with the straight-through gradient.  The forward quantises X into saved_x and W into saved_w, in every
  * direction that has buffers: the ones for the backward pass may be left out (serving).  `reuse`: FP4_REUSE_X /
  * FP4_REUSE_W -- that operand is there already (x or w may then be NULL).  saved_x and saved_w have the same
- * format, FP4_MX_E2M1 or FP4_MX_NVFP4.  dx or dw may be NULL.  `flags` of the backward: FP4_MX_ACCUMULATE_DX /
+ * format, FP4_MX_E2M1 or FP4_MX_NVFP4, and are two tensors with an amax each, unless both are reused.  dx or dw
+ * may be NULL.  `flags` of the backward: FP4_MX_ACCUMULATE_DX /
  * _DW add to what is there (a sum over consumers or micro-batches).
  */
 #define FP4_REUSE_X FP4_REUSE_A

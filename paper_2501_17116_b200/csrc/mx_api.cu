@@ -73,6 +73,16 @@ int quantize(fp4_ctx* ctx, cudaStream_t st, const Quantize* what, int n, int32_t
   return some ? launch_mx_quantize(ctx, st, todo, some, status) : FP4_OK;
 }
 
+// `rows` rows of `width` bytes; those further apart than a two-dimensional memset reaches (few, then) one by one.
+int clear(cudaStream_t st, char* p, int64_t pitch, int64_t width, int64_t rows) {
+  if (pitch <= MOST) {
+    FP4_CUDA_TRY(cudaMemset2DAsync(p, size_t(pitch), 0, size_t(width), size_t(rows), st));
+    return FP4_OK;
+  }
+  for (int64_t r = 0; r < rows; ++r) FP4_CUDA_TRY(cudaMemsetAsync(p + r * pitch, 0, size_t(width), st));
+  return FP4_OK;
+}
+
 // a b^T over I x J results and a contraction of C, up to two.
 struct Gemm {
   const fp4_mx_tensor* a;
@@ -92,7 +102,10 @@ int gemm(fp4_ctx* ctx, cudaStream_t st, const Gemm* what, int n, int32_t* status
     const MxMatrix o = matrix(g.out, g.I, g.J);
     const int64_t elt = g.out->dtype == FP4_DTYPE_FP32 ? 4 : 2;
     if (g.C == 0) {
-      if (!g.accumulate) FP4_CUDA_TRY(cudaMemset2DAsync(g.out->data, size_t(o.ld * elt), 0, size_t(g.J * elt), size_t(g.I), st));
+      if (!g.accumulate) {
+        const int rc = clear(st, static_cast<char*>(g.out->data), o.ld * elt, g.J * elt, g.I);
+        if (rc != FP4_OK) return rc;
+      }
       continue;
     }
     todo[some++] = {g.a_t ? g.a->codes_t : g.a->codes, g.a_t ? g.a->scales_t : g.a->scales, g.b_t ? g.b->codes_t : g.b->codes,
@@ -202,6 +215,8 @@ int fp4_mx_linear_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, const 
   if (!saved_x->codes || !saved_w->codes_t) return FP4_ERR_NULL;
   if ((!reuse_x && (!x || (!x->data && M && K))) || (!reuse_w && (!w || (!w->data && K && N))) || (!y->data && M && N)) return FP4_ERR_NULL;
   if (saved_x->format != saved_w->format) return FP4_ERR_ARG;
+  // (one tensor, or one amax, for both: only where neither is written)
+  if ((saved_x == saved_w || (saved_x->format == FP4_MX_NVFP4 && saved_x->amax == saved_w->amax)) && !(reuse_x && reuse_w)) return FP4_ERR_ARG;
   if ((reuse_x && (saved_x->rows != M || saved_x->cols != K)) || (reuse_w && (saved_w->rows != K || saved_w->cols != N))) return FP4_ERR_RANGE;
   if (!reuse_x) rc = check_matrix(x, M, K);
   if (rc == FP4_OK && !reuse_w) rc = check_matrix(w, K, N);
@@ -291,6 +306,7 @@ int fp4_mx_swiglu_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* gate, con
   if (rc == FP4_OK && (gate->dtype != up->dtype || (wanted(h) && h->dtype != gate->dtype))) rc = FP4_ERR_ARG;
   if (rc == FP4_OK && ckpt_gate) rc = check_checkpoint(ckpt_gate);
   if (rc == FP4_OK && ckpt_up) rc = check_checkpoint(ckpt_up);
+  if (rc == FP4_OK && ckpt_gate && ckpt_gate == ckpt_up) rc = FP4_ERR_ARG;
   if (rc == FP4_OK) rc = check_swiglu_quantized(quantized);
   if (rc != FP4_OK) return rc;
   for (fp4_mx_tensor* q : {ckpt_gate, ckpt_up, quantized})

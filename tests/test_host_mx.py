@@ -152,3 +152,20 @@ def test_swiglu_refusals(lib, ctx):
     assert bwd(mat(), ck(), ck(cols=65), mat(), mat()) == RANGE and bwd(mat(), ck(), ck(), mat(ld=1), mat()) == RANGE
     assert bwd(mat(), ck(), ck(), mat(dtype=1), mat()) == ARG and bwd(mat(), ck(), ck(), mat(), mat(), h=mat(dtype=1)) == ARG
     assert bwd(mat(), ck(), ten(R, K), mat(), mat()) == ARG
+
+
+@no_gpu
+def test_one_tensor_in_two_places_is_refused(lib, ctx):
+    """What a call writes twice: the second size would not fit the first one's buffers."""
+    fwd = lambda x, w, sx, sw, reuse: lib.fp4_mx_linear_fwd(ctx, None, ref(x), ref(w), 64, 64, 64, reuse, ref(mat()), ref(sx), ref(sw), P)   # noqa: E731
+    q = ten(64, 64)
+    assert passes(fwd(mat(), mat(), q, ten(64, 64), 0)) and passes(fwd(None, None, q, q, 3))
+    assert fwd(mat(), mat(), q, q, 0) == ARG and fwd(mat(), None, q, q, 1) == ARG and fwd(None, mat(), q, q, 2) == ARG
+    one, other = ten(64, 64, fmt=1), ten(64, 64, fmt=1)
+    assert fwd(mat(), mat(), one, other, 0) == ARG and fwd(mat(), None, one, other, 1) == ARG      # one amax for both
+    other.amax = P + 4
+    assert passes(fwd(mat(), mat(), one, other, 0))
+    ck = ten(8, 64, fmt=2, codes_t=False)
+    assert lib.fp4_mx_swiglu_fwd(ctx, None, ref(mat()), ref(mat()), 8, 64, None, ref(ck), ref(ck), None, P) == ARG
+    gemm = lambda a, b: lib.fp4_mx_gemm(ctx, None, ref(a), ref(b), 0, ref(mat()), P)              # noqa: E731
+    assert passes(gemm(q, q))                                                                  # (only read: as good as two)
