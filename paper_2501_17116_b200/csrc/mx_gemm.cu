@@ -88,6 +88,16 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// The last copies of a ring's producer have landed (or were given a millisecond each): a CTA must not leave ahead of them, whoever of it gave up.
+// In the ordinary course they have when the last MMA is issued.
+__device__ __forceinline__ void await_fills(uint64_t* full_bar, int stages, uint32_t fills) {
+  for (uint32_t f = fills < uint32_t(stages) ? 0u : fills - uint32_t(stages); f < fills; ++f) {
+    const uint64_t t0 = global_timer_ns();
+    while (!mbar_try_wait(&full_bar[f % uint32_t(stages)], (f / uint32_t(stages)) & 1u))
+      if (global_timer_ns() - t0 > 1000000ull) break;
+  }
+}
+
 // One k-block: its scales to tensor memory, then four MMAs.  `sfb_cols`: columns of B's scales per tile; `sfb_shift`: 2 where the
 // tile's columns begin with the second half of a scale tile.
 template <int FMT, int CTAS>
@@ -436,6 +446,7 @@ struct GemmArgs {
   uint32_t tx_bytes, idesc;
   int32_t* status;
   uint64_t wait_limit_ns;
+  int skip_fill;               // fp4_debug_set
 };
 constexpr int FIXED_SMEM = 1024 + MISC_BYTES + EPI_WARPS * STAGE_OUT;
 
@@ -480,7 +491,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
     fence_async_smem();
   }
   const uint32_t full0 = PAIR ? cluster_address(full_bar, 0) : smem_u32(full_bar);      // (a pair's copies complete on the even CTA's)
-  const auto request = [&](const Problem& q, int m_blk, int n0, int kb, int stage) {
+  const auto request = [&](const Problem& q, int m_blk, int n0, int kb, int stage, uint32_t fill) {
+    if (blockIdx.x == 0 && int(fill) == args.skip_fill) return;            // a left-out fill: no copy, no arrival
     uint8_t* p = smem + stage * STAGE_BYTES;
     const uint32_t bar = full0 + 8 * stage;
     if (rank == 0) mbar_arrive_expect_tx(&full_bar[stage], CTAS * args.tx_bytes);
@@ -496,7 +508,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
   if (!PAIR && threadIdx.x == 0 && worker < num_tiles) {
     const Problem& q = args.p[worker >= tiles_first];
     const int tt = worker - (worker >= tiles_first ? tiles_first : 0);
-    for (int s = 0; s < STAGES && s < q.num_k_blocks; ++s) request(q, tt % q.num_m_blocks, tt / q.num_m_blocks * args.bn, s, s);
+    for (int s = 0; s < STAGES && s < q.num_k_blocks; ++s) request(q, tt % q.num_m_blocks, tt / q.num_m_blocks * args.bn, s, s, uint32_t(s));
   }
   tc_fence_before();
   __syncthreads();
@@ -519,7 +531,7 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
           if (PAIR || t != worker || kb >= STAGES) {            // (those are on their way)
             ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
             if (!ok) break;
-            request(q, m_blk, n0, kb, stage);
+            request(q, m_blk, n0, kb, stage, fills);
           }
           ++fills;
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -536,16 +548,8 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
         // Gave up: the peer's copies complete on the even CTA's barriers too, so the copies in flight are given time to land.
         const uint64_t t0 = global_timer_ns();
         while (global_timer_ns() - t0 < 1000000ull) {}
-      } else if (!ok) {
-        const uint32_t last = fills < uint32_t(STAGES) ? fills : uint32_t(STAGES);
-        for (uint32_t back = 1; back <= last; ++back) {
-          const uint32_t f = fills - back;
-          const uint64_t t0 = global_timer_ns();
-          while (!mbar_try_wait(&full_bar[f % STAGES], (f / STAGES) & 1u)) {
-            if (global_timer_ns() - t0 > 1000000ull) break;
-          }
-        }
       }
+      if (!PAIR) await_fills(full_bar, STAGES, fills);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer ---------
@@ -638,6 +642,7 @@ struct FewArgs {
   Powers powers;
   int32_t* status;
   uint64_t wait_limit_ns;
+  int skip_fill;
 };
 __device__ __forceinline__ float4 load_cluster(uint32_t addr) {
   float4 v;
@@ -691,7 +696,8 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
   }
-  const auto request = [&](int kb, int stage) {
+  const auto request = [&](int kb, int stage, uint32_t fill) {
+    if (blockIdx.x == 0 && int(fill) == args.skip_fill) return;
     uint8_t* p = smem + stage * STAGE_BYTES;
     mbar_arrive_expect_tx(&full_bar[stage], args.tx_bytes);
     tma_load_2d(p, &map_w, &full_bar[stage], kb * 128, j_blk * BM);
@@ -703,7 +709,7 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   mx_wait_for_inputs();
   // The stages are empty and the barriers this thread's own work: the first k-blocks travel while the others meet.
   if (threadIdx.x == 0)
-    for (int s = 0, kb = rank; s < STAGES && kb < args.num_k_blocks; ++s, kb += args.splits) request(kb, s);
+    for (int s = 0, kb = rank; s < STAGES && kb < args.num_k_blocks; ++s, kb += args.splits) request(kb, s, uint32_t(s));
   tc_fence_before();
   __syncthreads();
   mx_let_next_start();
@@ -719,21 +725,12 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         if (fills >= uint32_t(STAGES)) {
           ok = mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, args.status, args.wait_limit_ns);
           if (!ok) break;
-          request(kb, stage);
+          request(kb, stage, fills);
         }
         ++fills;
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
       }
-      if (!ok) {
-        const uint32_t last = fills < uint32_t(STAGES) ? fills : uint32_t(STAGES);
-        for (uint32_t back = 1; back <= last; ++back) {
-          const uint32_t f = fills - back;
-          const uint64_t t0 = global_timer_ns();
-          while (!mbar_try_wait(&full_bar[f % STAGES], (f / STAGES) & 1u)) {
-            if (global_timer_ns() - t0 > 1000000ull) break;
-          }
-        }
-      }
+      await_fills(full_bar, STAGES, fills);
     }
   } else if (warp == 1) {
     if (elect_one()) {
@@ -916,6 +913,7 @@ int launch_tiles_as(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, i
   args.idesc = idesc_mx(FMT, CTAS * BM, bn);
   args.status = status;
   args.wait_limit_ns = wait_limit(ctx);
+  args.skip_fill = ctx->debug_skip_fill;
   int64_t tiles = 0;
   for (int i = 0; i < n; ++i) {
     Problem& p = args.p[i];
@@ -980,6 +978,7 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, i
   args.powers = powers_of(g);
   args.status = status;
   args.wait_limit_ns = wait_limit(ctx);
+  args.skip_fill = ctx->debug_skip_fill;
   int rc = make_codes_map(ctx, &w, g.b, g.J, g.C, BM);
   if (rc == FP4_OK) rc = make_codes_map(ctx, &x, g.a, g.I, g.C, args.nt);
   if (rc == FP4_OK) rc = make_scales_map(ctx, &sw, g.b_scales, g.J, g.C, FMT, 1);

@@ -660,3 +660,112 @@ def test_offsets_beyond_32_bits(lib, ctx):
     two = torch.as_strided(flat, (2, 300), (2 ** 31 - 512 * 8192, 1))
     two.copy_(draw(2, 300, "bf16", 5))
     check_quantized(lib.fp4_mx_quantize(ctx, two, lib.FP4_MX_E2M1, True, True), two.contiguous(), "mxfp4")
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+@pytest.mark.parametrize("I,J,C,fill", [(5, 640, 4096, 2), (5, 640, 512, 0), (256, 384, 512, 1), (1024, 1024, 4096, 9), (2048, 1920, 4096, 3),
+                                        (4096, 1920, 4096, 20)])
+def test_a_copy_that_never_comes_ends_the_kernel(lib, fmt, I, J, C, fill):
+    """A copy is left out, so that every role's wait runs out: the kernel returns and says so, and the next call is sound.  Few rows, tiles of
+    one CTA (a tile's first copies, which go ahead, and later ones) and of pairs."""
+    c = lib.Context(0, 0)
+    a = lib.fp4_mx_quantize(c, draw(I, C, "bf16", 1), fmt_of(lib, fmt))
+    b = lib.fp4_mx_quantize(c, draw(J, C, "bf16", 2), fmt_of(lib, fmt))
+    want = lib.fp4_mx_gemm(c, a, b)
+    torch.cuda.synchronize()
+    assert c.read_status() == 0
+    c.debug_set(lib.binding.FP4_DEBUG_WAIT_LIMIT_US, 1000)
+    c.debug_set(lib.binding.FP4_DEBUG_SKIP_FILL, fill)
+    guard = torch.full((I + 2, J + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    lib.fp4_mx_gemm(c, a, b, out=guard[1:-1, :J])
+    torch.cuda.synchronize()
+    assert c.read_status() & lib.FP4_DEV_TIMEOUT
+    assert (guard[0] == 7).all() and (guard[-1] == 7).all() and (guard[:, J:] == 7).all()
+    c.debug_set(lib.binding.FP4_DEBUG_SKIP_FILL, -1)
+    c.debug_set(lib.binding.FP4_DEBUG_WAIT_LIMIT_US, 0)
+    c.status.zero_()
+    again = lib.fp4_mx_gemm(c, a, b)
+    torch.cuda.synchronize()
+    assert c.read_status() == 0 and torch.equal(again, want)
+    c.close()
+
+
+def test_empty_contraction_over_rows_far_apart(lib, ctx):
+    """Zeros in rows 2^32 bytes apart, and nothing else touched."""
+    a, b = (lib.fp4_mx_quantize(ctx, torch.empty((r, 0), dtype=torch.bfloat16, device="cuda")) for r in (2, 5))
+    flat = torch.full(((1 << 30) + 16,), 3.0, device="cuda")
+    lib.fp4_mx_gemm(ctx, a, b, out=torch.as_strided(flat, (2, 5), (1 << 30, 1)))
+    assert (flat[:5] == 0).all() and (flat[5:64] == 3).all() and (flat[(1 << 30) - 64:1 << 30] == 3).all()
+    assert (flat[1 << 30:(1 << 30) + 5] == 0).all() and (flat[(1 << 30) + 5:] == 3).all()
+
+
+def test_operands_of_another_device_are_refused(lib, ctx):
+    on_cpu, x = lib.MXTensor(64, 128, "cpu", codes_t=True), draw(64, 128, "bf16", 1)
+    here = lib.fp4_mx_quantize(ctx, x, lib.FP4_MX_E2M1, True, True)
+    y, g = torch.empty((64, 64), device="cuda"), draw(64, 128, "bf16", 2)
+    kept = lib.SwigluCheckpoint(64, 128, "cpu")
+    for call in (lambda: lib.fp4_mx_quantize(ctx, x, out=on_cpu), lambda: lib.fp4_mx_dequantize(ctx, on_cpu),
+                 lambda: lib.fp4_mx_gemm(ctx, here, on_cpu, out=y), lambda: lib.fp4_mx_gemm(ctx, on_cpu, here, out=y),
+                 lambda: lib.fp4_mx_linear_fwd(ctx, x, x.T.contiguous(), saved_x=on_cpu),
+                 lambda: lib.fp4_mx_linear_fwd(ctx, x, x.T.contiguous(), saved_w=lib.MXTensor(128, 64, "cpu", codes_t=True)),
+                 lambda: lib.fp4_mx_linear_bwd(ctx, y, on_cpu, here), lambda: lib.fp4_mx_linear_bwd(ctx, y, here, on_cpu),
+                 lambda: lib.fp4_mx_swiglu_fwd(ctx, x, g, checkpoint=kept), lambda: lib.fp4_mx_swiglu_fwd(ctx, x, g, quantized=on_cpu),
+                 lambda: lib.fp4_mx_swiglu_bwd(ctx, x, kept)):
+        with pytest.raises(AssertionError, match="device"):
+            call()
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+def test_capture_that_forks_and_joins(lib, ctx, fmt):
+    """Two contexts quantise on two captured streams, which join ahead of the product; replayed twice, on new inputs."""
+    other, side = lib.Context(0, 0), torch.cuda.Stream()
+    x, w = draw(300, 640, "bf16", 1), draw(260, 640, "bf16", 2)
+    one = lambda: lib.MXTensor(300, 640, "cuda", fmt_of(lib, fmt))                            # noqa: E731
+    qx, qw, y = one(), lib.MXTensor(260, 640, "cuda", fmt_of(lib, fmt)), torch.empty((300, 260), device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            lib.fp4_mx_quantize(other, w, out=qw)
+        lib.fp4_mx_quantize(ctx, x, out=qx)
+        main.wait_stream(side)
+        lib.fp4_mx_gemm(ctx, qx, qw, out=y)
+    for trial in range(2):
+        x.copy_(draw(300, 640, "bf16", 3 + trial))
+        w.copy_(draw(260, 640, "bf16", 5 + trial))
+        graph.replay()
+        want = lib.fp4_mx_gemm(ctx, lib.fp4_mx_quantize(ctx, x, fmt_of(lib, fmt)), lib.fp4_mx_quantize(ctx, w, fmt_of(lib, fmt)), dtype=torch.float32)
+        assert torch.equal(y, want)
+    other.close()
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+@pytest.mark.parametrize("rows", [3, 300])
+def test_a_tensor_times_itself(lib, ctx, fmt, rows):
+    """x x^T from one tensor, and x^T x from its other direction."""
+    x = draw(rows, 200, "bf16", 1)
+    q, r = (lib.fp4_mx_quantize(ctx, x, fmt_of(lib, fmt), True, True) for _ in range(2))
+    for t in (False, True):
+        assert torch.equal(lib.fp4_mx_gemm(ctx, q, q, t, t, dtype=torch.float32), lib.fp4_mx_gemm(ctx, q, r, t, t, dtype=torch.float32))
+
+
+def test_host_threads_take_turns(lib, ctx):
+    """Four threads, one context, one stream: each has its own result."""
+    import threading
+    ins = [(draw(100 + 30 * i, 384, "bf16", 10 + i), draw(200, 384, "bf16", 20 + i)) for i in range(4)]
+    work = lambda x, w: lib.fp4_mx_gemm(ctx, lib.fp4_mx_quantize(ctx, x, lib.FP4_MX_NVFP4), lib.fp4_mx_quantize(ctx, w, lib.FP4_MX_NVFP4))   # noqa: E731
+    want, got = [work(x, w) for x, w in ins], [None] * 4
+    torch.cuda.synchronize()
+
+    def run(i):
+        for _ in range(20):
+            got[i] = work(*ins[i])
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
