@@ -76,6 +76,14 @@ def _matrix(ctx: Context, t):
     return _pack(t.data_ptr(), rows, _DTYPES[t.dtype], 0)
 
 
+def _tensor(ctx: Context, q):
+    """Reference to an operand's structure (None: of none)."""
+    if q is None:
+        return None
+    assert q.device == ctx.device, f"an operand on device {q.device}, the context on device {ctx.device}"
+    return q.ref
+
+
 def _new(ctx: Context, rows: int, cols: int, dtype):
     return torch.empty((rows, cols), dtype=dtype, device=f"cuda:{ctx.device}")
 
@@ -97,6 +105,7 @@ class MXTensor:
         self.struct = fp4_mx_tensor(rows, cols, where(self.codes), where(self.scales), where(self.codes_t), where(self.scales_t),
                                     _ptr(self.amax), fmt, 0)
         self.ref = C.byref(self.struct)
+        self.device = (self.codes if codes else self.codes_t).get_device() if codes or codes_t else -1
 
 
 class SwigluCheckpoint:
@@ -118,7 +127,7 @@ def fp4_mx_quantize(ctx: Context, x: torch.Tensor, fmt: int = FP4_MX_E2M1, codes
     if given:
         out.amax.copy_(amax.reshape(1))
         out.struct.flags = FP4_MX_AMAX_GIVEN
-    rc = ctx.lib.fp4_mx_quantize(ctx.handle, _stream_of(ctx.device), _matrix(ctx, x), out.ref, ctx.status.data_ptr())
+    rc = ctx.lib.fp4_mx_quantize(ctx.handle, _stream_of(ctx.device), _matrix(ctx, x), _tensor(ctx, out), ctx.status.data_ptr())
     if given:
         out.struct.flags = 0
     _check(rc)
@@ -132,7 +141,7 @@ def fp4_mx_dequantize(ctx: Context, q: MXTensor, transposed: bool = False, dtype
     if out is None:
         out = _new(ctx, *shape, dtype)
     assert out.shape == shape
-    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream_of(ctx.device), q.ref, int(transposed), _matrix(ctx, out),
+    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream_of(ctx.device), _tensor(ctx, q), int(transposed), _matrix(ctx, out),
                                      ctx.status.data_ptr()))
     return out
 
@@ -146,7 +155,7 @@ def fp4_mx_gemm(ctx: Context, a: MXTensor, b: MXTensor, a_t: bool = False, b_t: 
         out = _new(ctx, *shape, dtype)
     assert out.shape == shape
     flags = (FP4_MX_A_T if a_t else 0) | (FP4_MX_B_T if b_t else 0) | (FP4_MX_ACCUMULATE if accumulate else 0)
-    _check(ctx.lib.fp4_mx_gemm(ctx.handle, _stream_of(ctx.device), a.ref, b.ref, flags, _matrix(ctx, out), ctx.status.data_ptr()))
+    _check(ctx.lib.fp4_mx_gemm(ctx.handle, _stream_of(ctx.device), _tensor(ctx, a), _tensor(ctx, b), flags, _matrix(ctx, out), ctx.status.data_ptr()))
     return out
 
 
@@ -172,7 +181,7 @@ def fp4_mx_linear_fwd(ctx: Context, X: torch.Tensor | None, W: torch.Tensor | No
     reuse = (FP4_REUSE_X if reuse_x else 0) | (FP4_REUSE_W if reuse_w else 0)
     _check(ctx.lib.fp4_mx_linear_fwd(ctx.handle, _stream_of(ctx.device), None if reuse_x else _matrix(ctx, X),
                                      None if reuse_w else _matrix(ctx, W), M, K, N, reuse, _matrix(ctx, out),
-                                     saved_x.ref, saved_w.ref, ctx.status.data_ptr()))
+                                     _tensor(ctx, saved_x), _tensor(ctx, saved_w), ctx.status.data_ptr()))
     return out, saved_x, saved_w
 
 
@@ -190,7 +199,7 @@ def fp4_mx_linear_bwd(ctx: Context, dY: torch.Tensor, saved_x: MXTensor, saved_w
         dW = _new(ctx, K, N, dtype or dY.dtype)
     assert (dX is None or dX.shape == (M, K)) and (dW is None or dW.shape == (K, N))
     flags = (FP4_MX_ACCUMULATE_DX if accumulate_dx else 0) | (FP4_MX_ACCUMULATE_DW if accumulate_dw else 0)
-    _check(ctx.lib.fp4_mx_linear_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dY), saved_x.ref, saved_w.ref, M, K, N,
+    _check(ctx.lib.fp4_mx_linear_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dY), _tensor(ctx, saved_x), _tensor(ctx, saved_w), M, K, N,
                                      flags, _matrix(ctx, dX), _matrix(ctx, dW), ctx.status.data_ptr()))
     return dX, dW
 
@@ -205,10 +214,10 @@ def fp4_mx_swiglu_fwd(ctx: Context, gate: torch.Tensor, up: torch.Tensor, out: t
     g = u = q = None
     if checkpoint is not None:
         assert (checkpoint.gate.rows, checkpoint.gate.cols) == shape
-        g, u = checkpoint.gate.ref, checkpoint.up.ref
+        g, u = _tensor(ctx, checkpoint.gate), _tensor(ctx, checkpoint.up)
     if quantized is not None:
         assert (quantized.rows, quantized.cols) == shape
-        q = quantized.ref
+        q = _tensor(ctx, quantized)
     _check(ctx.lib.fp4_mx_swiglu_fwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, gate), _matrix(ctx, up), rows, cols,
                                      _matrix(ctx, out), g, u, q, ctx.status.data_ptr()))
     return out, checkpoint, quantized
@@ -224,7 +233,8 @@ def fp4_mx_swiglu_bwd(ctx: Context, dh: torch.Tensor, checkpoint: SwigluCheckpoi
     q = None
     if quantized is not None:
         assert (quantized.rows, quantized.cols) == shape
-        q = quantized.ref
-    _check(ctx.lib.fp4_mx_swiglu_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dh), checkpoint.gate.ref, checkpoint.up.ref, rows, cols,
+        q = _tensor(ctx, quantized)
+    _check(ctx.lib.fp4_mx_swiglu_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dh), _tensor(ctx, checkpoint.gate),
+                                     _tensor(ctx, checkpoint.up), rows, cols,
                                      _matrix(ctx, dgate), _matrix(ctx, dup), _matrix(ctx, h), q, ctx.status.data_ptr()))
     return dgate, dup

@@ -2,6 +2,7 @@
 they touch the device, and read nothing of the context before but its mutex: zeroed bytes stand in for one, and a call that
 passes all checks ends with the error of the missing device (or, on a GPU machine, is not made)."""
 import ctypes as C
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -169,3 +170,11 @@ def test_one_tensor_in_two_places_is_refused(lib, ctx):
     assert lib.fp4_mx_swiglu_fwd(ctx, None, ref(mat()), ref(mat()), 8, 64, None, ref(ck), ref(ck), None, P) == ARG
     gemm = lambda a, b: lib.fp4_mx_gemm(ctx, None, ref(a), ref(b), 0, ref(mat()), P)              # noqa: E731
     assert passes(gemm(q, q))                                                                  # (only read: as good as two)
+
+
+def test_binding_refuses_an_operand_of_another_device(lib):
+    q = fp4.MXTensor(4, 64, "cpu")
+    with pytest.raises(AssertionError, match="device"):
+        fp4.mx._tensor(SimpleNamespace(device=0), q)
+    assert fp4.mx._tensor(SimpleNamespace(device=-1), q) is q.ref                               # (torch's number for the CPU)
+    assert fp4.mx._tensor(SimpleNamespace(device=0), None) is None
