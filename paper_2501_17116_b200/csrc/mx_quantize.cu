@@ -884,14 +884,19 @@ __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_con
 }
 
 // -------------------------------------------------------------------------------- SwiGLU ---
-// h = g sigmoid(g) u in fp32, rounded once.  sigmoid(g) and 1 - sigmoid(g) = sigmoid(-g) from exp(-|g|), which cannot overflow:
-// neither loses its digits where it is small.
+// h = g sigmoid(g) u in fp32, rounded once.  sigmoid(g) and 1 - sigmoid(g) = sigmoid(-g) from exp(-|g|), which cannot overflow: neither loses its
+// digits where it is small.  Two approximate instructions and a square: exp(-|g|) to 2^-21 (and 2^-25 |g| from the exponent's rounding), the
+// reciprocal to 2^-23.
 struct Sigmoid {
   float s, rest;               // sigmoid(g), sigmoid(-g)
 };
 __device__ __forceinline__ Sigmoid sigmoid(float g) {
-  const float e = __expf(-fabsf(g)), r = __fdividef(1.0f, 1.0f + e), small = e * r;
-  return {g < 0.0f ? small : r, g < 0.0f ? r : small};
+  // exp(-|g|) as the square of 2^(-|g| log2(e) / 2), which is a normal number wherever its square is more than nothing
+  float h, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(h) : "f"(fabsf(g) * -0.7213475204444817f));
+  const float e = h * h;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return {(g < 0.0f ? e : 1.0f) * r, (g < 0.0f ? 1.0f : e) * r};
 }
 
 struct SwigluArgs {
