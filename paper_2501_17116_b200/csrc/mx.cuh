@@ -110,3 +110,6 @@ struct MxGemm {
 };
 // One product or two that do not depend on one another, none of them empty.
 int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, int32_t* status);
+// The product of few rows with an operand that is there, a's codes (one direction, and its amax) being made from `x` by the kernel itself.
+// `done`: false where that is not the faster way (nothing was launched).
+int launch_mx_linear_few(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize& x, const MxGemm& g, int32_t* status, bool* done);

@@ -93,6 +93,11 @@ struct Gemm {
   const fp4_mx_matrix* out;
   bool accumulate;
 };
+MxGemm mx_gemm(const Gemm& g) {
+  return {g.a_t ? g.a->codes_t : g.a->codes, g.a_t ? g.a->scales_t : g.a->scales, g.b_t ? g.b->codes_t : g.b->codes,
+          g.b_t ? g.b->scales_t : g.b->scales, g.a->amax, g.b->amax, g.I, g.J, g.C, g.a->format, g.out->data, matrix(g.out, g.I, g.J).ld,
+          g.out->dtype, g.accumulate};
+}
 int gemm(fp4_ctx* ctx, cudaStream_t st, const Gemm* what, int n, int32_t* status) {
   MxGemm todo[2];
   int some = 0;
@@ -108,8 +113,7 @@ int gemm(fp4_ctx* ctx, cudaStream_t st, const Gemm* what, int n, int32_t* status
       }
       continue;
     }
-    todo[some++] = {g.a_t ? g.a->codes_t : g.a->codes, g.a_t ? g.a->scales_t : g.a->scales, g.b_t ? g.b->codes_t : g.b->codes,
-                    g.b_t ? g.b->scales_t : g.b->scales, g.a->amax, g.b->amax, g.I, g.J, g.C, g.a->format, g.out->data, o.ld, g.out->dtype, g.accumulate};
+    todo[some++] = mx_gemm(g);
   }
   return some ? launch_mx_gemm(ctx, st, todo, some, status) : FP4_OK;
 }
@@ -237,9 +241,14 @@ int fp4_mx_linear_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, const 
     saved_x->cols = K;
     todo[n++] = {x, saved_x};
   }
+  const Gemm one = {saved_x, false, saved_w, true, M, N, K, y, false};
+  if (reuse_w && !reuse_x && M && N && K) {
+    bool done;
+    rc = launch_mx_linear_few(ctx, st, {matrix(x, M, K), x->dtype, saved_x}, mx_gemm(one), status, &done);
+    if (rc != FP4_OK || done) return rc;
+  }
   if (n) rc = quantize(ctx, st, todo, n, status);
   if (rc != FP4_OK) return rc;
-  const Gemm one = {saved_x, false, saved_w, true, M, N, K, y, false};
   return gemm(ctx, st, &one, 1, status);
 }
 

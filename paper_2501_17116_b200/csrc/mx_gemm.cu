@@ -15,7 +15,8 @@
 // stages, so that the results of a tile leave under the next one's MMAs.  `mx_gemm_few_kernel`: few rows (tokens), where the
 // weight's bytes and the latency count: the operands change places, so that 128 rows of the weight fill the instruction's rows
 // and the tokens its columns, and the CTAs of a cluster split the contraction and add their parts through distributed shared
-// memory in order of rank.
+// memory in order of rank.  Of very few tokens it takes the values themselves (a layer's forward pass onto weights that are there): each CTA
+// quantises what its k-blocks need while the weights travel, which saves the quantiser's launch and the wait for it.
 // Every wait is bounded: on a timeout a CTA raises FP4_DEV_TIMEOUT, drains its copies, frees its tensor memory and returns.
 #include <cuda.h>
 #include <cuda_fp16.h>
@@ -23,6 +24,7 @@
 #include <type_traits>
 
 #include "mx.cuh"
+#include "mx_codes.cuh"
 #include "tc_ptx.cuh"
 
 namespace {
@@ -631,10 +633,25 @@ __global__ void __launch_bounds__(THREADS, 1) mx_gemm_kernel(const __grid_consta
 // CTA `rank` of a cluster of `splits` takes k-blocks rank, rank + splits, ... of 128 weight rows (the instruction's rows) and all
 // tokens (its columns, `nt` of them, a multiple of 16).
 constexpr int FEW_ROWS = 128;                     // tokens at most: one scale tile
-constexpr int FEW_THREADS = 64 + 32 * 8;              // at most: 8 warps read the accumulators, 4 of up to 32 tokens
+constexpr int FEW_THREADS = 64 + 32 * 8;              // at most: 8 warps read the accumulators, 4 of up to 32 tokens that are an operand already
 constexpr int FEW_MAX_STAGES = 8;
 constexpr int FEW_LEAST_SMEM = 78 * 1024;
+constexpr int FEW_MISC = 512;
+constexpr int FEW_X_ROWS = 16;                    // tokens at most of which the kernel makes the operand itself, and a CTA's k-blocks then
+constexpr int FEW_X_BLOCKS = 16;
+constexpr int FEW_X_PARTS = 48;                   // tokens times k-blocks of a CTA
+// Tokens that are an operand not yet: the CTAs make what they need of it, those of the first weight rows write it down.
+struct FewX {
+  const void* p;
+  int64_t ld, cols;
+  uint8_t *codes, *scales;
+  uint32_t* amax;              // NVFP4
+  bool find;                   // amax is not there: every CTA looks for it
+  bool wide;                   // rows on 16-byte boundaries
+};
+__host__ __device__ constexpr int few_x_bytes(int fmt) { return FEW_X_ROWS * 128 + scale_bytes(fmt); }      // of a k-block
 struct FewArgs {
+  FewX x;
   int num_k_blocks, nt, splits;
   int stages, stage_bytes;
   uint32_t tx_bytes, idesc, tmem_cols;
@@ -667,20 +684,122 @@ __device__ __forceinline__ void put_four(const OutArgs& o, int row, int col, con
   else if (o.dtype == FP4_DTYPE_FP16) put_four_as<FP4_DTYPE_FP16>(o, row, col, f);
   else put_four_as<FP4_DTYPE_FP32>(o, row, col, f);
 }
-template <int FMT>
+// Eight elements of a row, those behind its end 0.
+template <class T>
+__device__ __forceinline__ void load_eight(const FewX& x, int row, int64_t col, uint32_t (&w)[2 * sizeof(T)]) {
+  const T* p = static_cast<const T*>(x.p) + row * x.ld + col;
+  if (x.wide && col + 8 <= x.cols) {
+#pragma unroll
+    for (int i = 0; i < int(sizeof(T)) / 2; ++i) {
+      const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+      w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t v = 0;
+      if (col + i < x.cols) {
+        if constexpr (sizeof(T) == 4) v = reinterpret_cast<const uint32_t*>(p)[i];
+        else v = reinterpret_cast<const unsigned short*>(p)[i];
+      }
+      if constexpr (sizeof(T) == 4) w[i] = v;
+      else w[i / 2] = i % 2 ? w[i / 2] | (v << 16) : v;
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ uint32_t amax_of_eight(const uint32_t (&w)[2 * sizeof(T)]) {
+  uint32_t m = w[0];
+#pragma unroll
+  for (int i = 1; i < 2 * int(sizeof(T)); ++i) m = mx_codes::TypeOf<T>::most(m, w[i]);
+  if constexpr (sizeof(T) == 4) return m & 0x7FFFFFFFu;
+  else return max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+}
+// Largest magnitude of the token, as a pattern of fp32, in every thread of warps 2 and up (`s_max`: a word for each).
+template <class T>
+__device__ __forceinline__ uint32_t few_amax(const FewX& x, uint32_t* s_max) {
+  const int threads = int(blockDim.x) - 64, t = int(threadIdx.x) - 64;
+  const int64_t pieces = (x.cols + 7) / 8;
+  uint32_t m = 0;
+  for (int64_t c = t; c < pieces; c += 4 * threads) {
+    uint32_t w[4][2 * sizeof(T)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_eight<T>(x, 0, (c + i * threads < pieces ? c + i * threads : c) * 8, w[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, amax_of_eight<T>(w[i]));
+  }
+  m = __reduce_max_sync(0xFFFFFFFFu, m);
+  if ((threadIdx.x & 31) == 0) s_max[(threadIdx.x >> 5) - 2] = m;
+  asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+  for (int i = 0; i < threads / 32; ++i) m = max(m, s_max[i]);
+  return __float_as_uint(mx_codes::TypeOf<T>::value(m));
+}
+// The tokens' operand by warps 2 and up, a token's part of a k-block at a time, eight elements a lane: codes as TMA would have brought them
+// (128-byte rows, swizzled), behind them the scales.  What stands for nothing is 0 already.  `note`: also to where the caller wants it.
+template <class T, int FMT>
+__device__ __forceinline__ void make_operand(const FewX& x, int rows, int blocks, int rank, int splits, float2 tensor, uint8_t* made, uint64_t* x_bar, bool note,
+                                             bool& bad) {
+  constexpr int LANES = mx_block(FMT) / 8, AT_ONCE = 4;      // lanes of a scale's block; parts on their way together
+  const int lane = threadIdx.x & 31, warps = int(blockDim.x) / 32 - 2, parts = blocks * rows;
+  const int64_t pitch = mx_pitch(x.cols, FMT), tiles = mx_scale_tiles(x.cols, FMT);
+#pragma unroll 1
+  for (int p0 = int(threadIdx.x >> 5) - 2; p0 < parts; p0 += AT_ONCE * warps) {
+    uint32_t w[AT_ONCE][2 * sizeof(T)];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int p = p0 + i * warps, n = p / rows;
+      if (p < parts) load_eight<T>(x, p - n * rows, int64_t(rank + n * splits) * 256 + lane * 8, w[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int p = p0 + i * warps, n = p / rows, r = p - n * rows, kb = rank + n * splits;
+      if (p >= parts) break;
+      uint8_t* to = made + n * few_x_bytes(FMT);
+      uint32_t m = amax_of_eight<T>(w[i]);
+#pragma unroll
+      for (int k = 1; k < LANES; k *= 2) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, k));
+      const mx_codes::Scale s = mx_codes::scale_of<T, FMT>(m, tensor);
+      bad |= !s.finite;
+      uint32_t codes;
+      const auto value = [&](int k) {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i][k]);
+        else return k % 2 ? mx_codes::TypeOf<T>::hi(w[i][k / 2]) : mx_codes::TypeOf<T>::lo(w[i][k / 2]);
+      };
+      mx_codes::encode_block<T, FMT, 8>(s, [&](int k) { return mx_codes::pack2(value(2 * k), value(2 * k + 1)); }, &codes);
+      const int at = mx_codes::scale_at(r, lane / LANES);
+      *reinterpret_cast<uint32_t*>(to + r * 128 + ((lane * 4) ^ ((r & 7) << 4))) = codes;
+      if (lane % LANES == 0) to[FEW_X_ROWS * 128 + at] = uint8_t(s.byte);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&x_bar[n]);
+      if (note) {
+        if (kb * 128 + lane * 4 < pitch) *reinterpret_cast<uint32_t*>(x.codes + r * pitch + kb * 128 + lane * 4) = codes;
+        if (lane % LANES == 0 && kb * scale_tiles(FMT) + at / 512 < tiles) x.scales[int64_t(kb) * scale_bytes(FMT) + at] = uint8_t(s.byte);
+      }
+    }
+  }
+}
+
+// T: type of the tokens where they are no operand yet, else void.
+template <int FMT, class T>
 __global__ void __launch_bounds__(FEW_THREADS)
 mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                    const __grid_constant__ CUtensorMap map_sw, const __grid_constant__ CUtensorMap map_sx,
                    const __grid_constant__ FewArgs args) {
+  constexpr bool MAKE = !std::is_void_v<T>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  const int STAGES = args.stages, STAGE_BYTES = args.stage_bytes, x_bytes = args.nt * 128;
-  uint8_t* misc = smem + STAGES * STAGE_BYTES;
+  // a stage: weights, tokens, the scales of either; or tokens and their scales, by k-block, behind the ring
+  const int STAGES = args.stages, STAGE_BYTES = args.stage_bytes, x_bytes = MAKE ? 0 : args.nt * 128;
+  uint8_t* x_made = smem + STAGES * STAGE_BYTES;
+  uint8_t* misc = x_made + (MAKE ? (args.num_k_blocks + args.splits - 1) / args.splits * few_x_bytes(FMT) : 0);
   uint64_t* full_bar = reinterpret_cast<uint64_t*>(misc);
   uint64_t* empty_bar = full_bar + FEW_MAX_STAGES;
   uint64_t* final_bar = empty_bar + FEW_MAX_STAGES;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(final_bar + 1);
+  uint64_t* x_bar = final_bar + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(x_bar + FEW_X_BLOCKS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* s_amax = tmem_slot + 2;                        // the tokens' amax, then one word a warp
   const int warp = __shfl_sync(0xFFFFFFFFu, int(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   const int rank = args.splits > 1 ? int(cluster_ctarank()) : 0;
@@ -692,6 +811,8 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       mbar_init(&empty_bar[s], 1);
     }
     mbar_init(final_bar, 1);
+    if (MAKE)
+      for (int i = 0; i < FEW_X_BLOCKS; ++i) mbar_init(&x_bar[i], uint32_t(args.out.I));
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_smem();
@@ -702,11 +823,25 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     mbar_arrive_expect_tx(&full_bar[stage], args.tx_bytes);
     tma_load_2d(p, &map_w, &full_bar[stage], kb * 128, j_blk * BM);
     tma_load_2d(p + A_BYTES + x_bytes, &map_sw, &full_bar[stage], kb * (scale_bytes(FMT) / 8), j_blk);
-    tma_load_2d(p + A_BYTES, &map_x, &full_bar[stage], kb * 128, 0);
-    tma_load_2d(p + A_BYTES + x_bytes + scale_bytes(FMT), &map_sx, &full_bar[stage], kb * (scale_bytes(FMT) / 8), 0);
+    if (!MAKE) {
+      tma_load_2d(p + A_BYTES, &map_x, &full_bar[stage], kb * 128, 0);
+      tma_load_2d(p + A_BYTES + x_bytes + scale_bytes(FMT), &map_sx, &full_bar[stage], kb * (scale_bytes(FMT) / 8), 0);
+    }
   };
   if (warp == 1) tmem_alloc<1>(tmem_slot, args.tmem_cols);
+  if (MAKE) {
+    for (int i = threadIdx.x; i < int(misc - x_made) / 16; i += int(blockDim.x)) reinterpret_cast<uint4*>(x_made)[i] = make_uint4(0, 0, 0, 0);
+    fence_async_smem();
+  }
   mx_wait_for_inputs();
+  if (MAKE && j_blk == 0) {
+    // scales that stand for no token
+    const int64_t words = mx_scale_tiles(args.x.cols, FMT) * 128;
+    for (int64_t i = rank * int(blockDim.x) + int(threadIdx.x); i < words; i += args.splits * int(blockDim.x)) {
+      const int row = int(i % 4) * 32 + int(i / 4) % 32;
+      if (row >= args.out.I) reinterpret_cast<uint32_t*>(args.x.scales)[i] = 0;
+    }
+  }
   // The stages are empty and the barriers this thread's own work: the first k-blocks travel while the others meet.
   if (threadIdx.x == 0)
     for (int s = 0, kb = rank; s < STAGES && kb < args.num_k_blocks; ++s, kb += args.splits) request(kb, s, uint32_t(s));
@@ -734,15 +869,16 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     }
   } else if (warp == 1) {
     if (elect_one()) {
-      int stage = 0;
+      int stage = 0, n = 0;
       uint32_t phase = 0, sf = 0;
       bool ok = true;
-      for (int kb = rank; kb < args.num_k_blocks; kb += args.splits) {
-        ok = mbar_wait(&full_bar[stage], phase, abort_flag, args.status, args.wait_limit_ns);
+      for (int kb = rank; kb < args.num_k_blocks; kb += args.splits, ++n) {
+        if (MAKE) ok = mbar_wait(&x_bar[n], 0, abort_flag, args.status, args.wait_limit_ns);
+        ok = ok && mbar_wait(&full_bar[stage], phase, abort_flag, args.status, args.wait_limit_ns);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t p = smem_u32(smem + stage * STAGE_BYTES);
-        issue_k_block<FMT, 1>(p, p + A_BYTES, p + A_BYTES + x_bytes, p + A_BYTES + x_bytes + scale_bytes(FMT), 1, tmem_base,
+        const uint32_t p = smem_u32(smem + stage * STAGE_BYTES), x = MAKE ? smem_u32(x_made + n * few_x_bytes(FMT)) : p + A_BYTES;
+        issue_k_block<FMT, 1>(p, x, p + A_BYTES + x_bytes, MAKE ? x + FEW_X_ROWS * 128 : p + A_BYTES + x_bytes + scale_bytes(FMT), 1, tmem_base,
                               tmem_base + FEW_ROWS + sf * sf_cols(FMT), 0, args.idesc, kb == rank);
         sf ^= 1u;
         tc_commit<1>(&empty_bar[stage]);
@@ -751,6 +887,22 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
       tc_commit<1>(final_bar);
     }
     __syncwarp();
+  } else if constexpr (MAKE) {
+    // ------------------------------------------------------------------ the tokens' operand ----
+    const FewX& x = args.x;
+    float2 tensor = make_float2(1.0f, 1.0f);
+    if (FMT == FP4_MX_NVFP4) {
+      const uint32_t m = x.find ? few_amax<T>(x, s_amax + 1) : __ldg(x.amax);
+      const int k = mx_tensor_exponent(m);
+      tensor = make_float2(mx_codes::pow2_int(k), mx_codes::pow2_int(-k));
+      if (threadIdx.x == 64) {
+        *s_amax = m;
+        if (x.find && blockIdx.x == 0) *x.amax = m;
+      }
+    }
+    bool bad = false;
+    make_operand<T, FMT>(x, args.out.I, (args.num_k_blocks - rank + args.splits - 1) / args.splits, rank, args.splits, tensor, x_made, x_bar, j_blk == 0, bad);
+    if (__any_sync(0xFFFFFFFFu, bad) && j_blk == 0 && lane == 0) atomicOr(args.status, FP4_DEV_NONFINITE);
   }
   // Every thread awaits the last MMA (of a CTA without a k-block: at once).
   const bool done = __all_sync(0xFFFFFFFFu, mbar_wait(final_bar, 0, abort_flag, args.status, args.wait_limit_ns));
@@ -772,7 +924,13 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (args.splits > 1) cluster_sync_all();
-  const float2 scales = tensor_scales(args.powers);
+  float2 scales = make_float2(1.0f, 1.0f);
+  if (MAKE && FMT == FP4_MX_NVFP4) {
+    scales.x = mx_codes::pow2_int(mx_tensor_exponent(*s_amax));
+    scales.y = mx_codes::pow2_int(mx_tensor_exponent(__ldg(args.powers.b)));
+  } else {
+    scales = tensor_scales(args.powers);
+  }
   // four neighbouring columns of a token at a time, and four such fours on their way together
   constexpr int AT_ONCE = 4;
   const int step = args.splits * int(blockDim.x), n = args.out.I * (BM / 4);
@@ -955,19 +1113,21 @@ int launch_tiles(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, cons
 #undef AS
 }
 
-template <int FMT>
-int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, int32_t* status) {
-  CUtensorMap w, x, sw, sx;
+template <int FMT, class T = void>
+int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, int32_t* status, const FewX* from = nullptr) {
+  constexpr bool MAKE = !std::is_void_v<T>;
+  CUtensorMap w, x = {}, sw, sx = {};
   FewArgs args = {};
   args.num_k_blocks = int((g.C + 255) / 256);
   args.nt = int((g.I + 15) / 16 * 16);
   const int tiles = int((g.J + BM - 1) / BM);
   args.splits = splits;
-  args.stage_bytes = A_BYTES + args.nt * 128 + 2 * scale_bytes(FMT);
-  // (more CTAs than SMs: two on each)
-  args.stages = ((tiles * splits > ctx->num_sms ? 113 * 1024 : MOST_SMEM) - 1024 - MISC_BYTES) / args.stage_bytes;
-  if (args.stages > FEW_MAX_STAGES) args.stages = FEW_MAX_STAGES;
   const int per_cta = (args.num_k_blocks + args.splits - 1) / args.splits;
+  args.stage_bytes = A_BYTES + (MAKE ? scale_bytes(FMT) : args.nt * 128 + 2 * scale_bytes(FMT));
+  const int fixed = 1024 + FEW_MISC + (MAKE ? per_cta * few_x_bytes(FMT) : 0);
+  // (more CTAs than SMs: two on each)
+  args.stages = ((tiles * splits > ctx->num_sms ? 113 * 1024 : MOST_SMEM) - fixed) / args.stage_bytes;
+  if (args.stages > FEW_MAX_STAGES) args.stages = FEW_MAX_STAGES;
   if (args.stages > per_cta) args.stages = per_cta;
   // (the parts of the result, 512 bytes a token, go over the ring)
   while (args.stages * args.stage_bytes < args.nt * BM * 4) ++args.stages;
@@ -979,19 +1139,20 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, i
   args.status = status;
   args.wait_limit_ns = wait_limit(ctx);
   args.skip_fill = ctx->debug_skip_fill;
+  if (MAKE) args.x = *from;
   int rc = make_codes_map(ctx, &w, g.b, g.J, g.C, BM);
-  if (rc == FP4_OK) rc = make_codes_map(ctx, &x, g.a, g.I, g.C, args.nt);
   if (rc == FP4_OK) rc = make_scales_map(ctx, &sw, g.b_scales, g.J, g.C, FMT, 1);
-  if (rc == FP4_OK) rc = make_scales_map(ctx, &sx, g.a_scales, g.I, g.C, FMT, 1);
+  if (rc == FP4_OK && !MAKE) rc = make_codes_map(ctx, &x, g.a, g.I, g.C, args.nt);
+  if (rc == FP4_OK && !MAKE) rc = make_scales_map(ctx, &sx, g.a_scales, g.I, g.C, FMT, 1);
   if (rc != FP4_OK) return rc;
-  constexpr auto kernel = mx_gemm_few_kernel<FMT>;
+  constexpr auto kernel = mx_gemm_few_kernel<FMT, T>;
   FP4_CUDA_TRY(mx_allow_smem<kernel>(ctx->device, MOST_SMEM));
   // At least a third of an SM's shared memory: two CTAs an SM find their 256 columns of tensor memory, a third one would wait for
   // theirs, and CTAs of clusters that wait so for one another would wait for good.
-  int smem = 1024 + MISC_BYTES + args.stages * args.stage_bytes;
+  int smem = fixed + args.stages * args.stage_bytes;
   if (smem < FEW_LEAST_SMEM) smem = FEW_LEAST_SMEM;
   KernelScope scope(ctx, stream, KC_GEMM, 1);
-  return mx_launch<kernel>(dim3(unsigned(tiles * args.splits)), args.nt <= 32 ? FEW_THREADS - 128 : FEW_THREADS, smem, args.splits, stream, w, x, sw, sx, args);
+  return mx_launch<kernel>(dim3(unsigned(tiles * args.splits)), args.nt <= 32 && !MAKE ? FEW_THREADS - 128 : FEW_THREADS, smem, args.splits, stream, w, x, sw, sx, args);
 }
 
 }  // namespace
@@ -1017,4 +1178,29 @@ int launch_mx_gemm(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, in
     if (few.cost <= f.cost) return nv ? launch_few<FP4_MX_NVFP4>(ctx, stream, *g, few.splits, status) : launch_few<FP4_MX_E2M1>(ctx, stream, *g, few.splits, status);
   }
   return nv ? launch_tiles<FP4_MX_NVFP4>(ctx, stream, g, 1, f, status) : launch_tiles<FP4_MX_E2M1>(ctx, stream, g, 1, f, status);
+}
+
+int launch_mx_linear_few(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize& x, const MxGemm& g, int32_t* status, bool* done) {
+  const bool nv = g.format == FP4_MX_NVFP4;
+  const int elt = x.dtype == FP4_DTYPE_FP32 ? 4 : 2;
+  *done = false;
+  if (g.I > FEW_X_ROWS || x.q->codes_t) return FP4_OK;
+  const FewForm few = choose_few(ctx, g);
+  if (few.cost > choose_form(ctx, &g, 1).cost) return FP4_OK;
+  // A launch and its wait against what every CTA does again.  Tokens x contraction x weight rows, us, made by the kernel / by the quantiser:
+  // 1 x 4096 x 11008 8.8 / 10.1, 4 x 11008 x 4096 9.9 / 10.9 (44 parts), 6 x 4096 x 11008 9.8 / 10.1 (48), 8 x 4096 x 11008 10.5 / 9.4 (64).
+  const int64_t per_cta = ((g.C + 255) / 256 + few.splits - 1) / few.splits;
+  if (per_cta > FEW_X_BLOCKS || g.I * per_cta > FEW_X_PARTS) return FP4_OK;
+  // Where every CTA has to look for the amax first: 1 x 13824 x 5120 13.0 / 14.9, 1 x 4096 x 4096 7.6 / 8.5, 2 x 4096 x 11008 11.5 / 10.5.
+  const bool find = nv && !(x.q->flags & FP4_MX_AMAX_GIVEN);
+  if (find && g.I > 1) return FP4_OK;
+  *done = true;
+  const FewX from = {x.x.p, x.x.ld, g.C, x.q->codes, x.q->scales, reinterpret_cast<uint32_t*>(x.q->amax), find,
+                     (reinterpret_cast<uintptr_t>(x.x.p) & 15) == 0 && (x.x.ld * elt) % 16 == 0};
+#define FROM(T) \
+  (nv ? launch_few<FP4_MX_NVFP4, T>(ctx, stream, g, few.splits, status, &from) : launch_few<FP4_MX_E2M1, T>(ctx, stream, g, few.splits, status, &from))
+  if (x.dtype == FP4_DTYPE_BF16) return FROM(__nv_bfloat16);
+  if (x.dtype == FP4_DTYPE_FP16) return FROM(__half);
+  return FROM(float);
+#undef FROM
 }

@@ -769,3 +769,60 @@ def test_host_threads_take_turns(lib, ctx):
         t.join()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+@pytest.mark.parametrize("dt", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("M,K,N", [(1, 1, 5), (1, 40, 130), (1, 4096, 700), (3, 1000, 129), (5, 2051, 640), (16, 384, 256), (16, 8192, 512), (17, 512, 300),
+                                   (2, 13824, 4096), (1, 33000, 200)])
+def test_few_tokens_onto_weights_that_are_there(lib, ctx, fmt, dt, M, K, N):
+    """Serving: the tokens' operand is made beside the product, or ahead of it; both give the codes, scales, amax and results of the two calls."""
+    f = fmt_of(lib, fmt)
+    w = lib.fp4_mx_quantize(ctx, draw(K, N, "bf16", K + N), f, codes=False, codes_t=True)
+    for seed, (ld, skip) in enumerate(((K, 0), (K + 8, 8), (K + 3, 1))):
+        x = torch.zeros((M, ld), dtype=DT[dt], device="cuda")[:, skip:]
+        x = x[:, :K] if x.shape[1] >= K else torch.zeros((M, ld + skip), dtype=DT[dt], device="cuda")[:, skip:skip + K]
+        x.copy_(draw(M, K, dt, 7 * seed + M))
+        want = lib.fp4_mx_quantize(ctx, x, f)
+        saved = lib.MXTensor(M, K, "cuda", f)
+        for t in (saved.codes, saved.scales):
+            t.fill_(0xAA)
+        ctx.status.zero_()
+        y, _, _ = lib.fp4_mx_linear_fwd(ctx, x, None, f, saved, w, reuse_w=True, dtype=torch.float32)
+        assert torch.equal(saved.codes, want.codes) and torch.equal(saved.scales, want.scales)
+        assert fmt == "mxfp4" or torch.equal(saved.amax, want.amax)
+        assert torch.equal(y, lib.fp4_mx_gemm(ctx, want, w, b_t=True, dtype=torch.float32))
+        assert ctx.read_status() == 0
+    out = torch.full((M, N + 5), 9.0, dtype=torch.bfloat16, device="cuda")                      # results off 16-byte boundaries
+    lib.fp4_mx_linear_fwd(ctx, x, None, f, saved, w, reuse_w=True, out=out[:, 1:N + 1])
+    assert torch.equal(out[:, 1:N + 1], y.bfloat16()) and (out[:, 0] == 9).all() and (out[:, N + 1:] == 9).all()
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_few_tokens_with_a_non_finite_value(lib, ctx, fmt, bad):
+    f, M, K, N = fmt_of(lib, fmt), 4, 700, 260
+    w = lib.fp4_mx_quantize(ctx, draw(K, N, "bf16", 1), f, codes=False, codes_t=True)
+    x = draw(M, K, "bf16", 2)
+    x[2, 555] = bad
+    want, saved = lib.fp4_mx_quantize(ctx, x, f), lib.MXTensor(M, K, "cuda", f)
+    ctx.status.zero_()
+    y, _, _ = lib.fp4_mx_linear_fwd(ctx, x, None, f, saved, w, reuse_w=True)
+    assert ctx.read_status() == lib.FP4_DEV_NONFINITE
+    ctx.status.zero_()
+    assert torch.equal(saved.codes, want.codes) and torch.equal(saved.scales, want.scales)
+    assert y[2].isnan().all() and y[[0, 1, 3]].isfinite().all()
+
+
+def test_few_tokens_with_a_given_amax(lib, ctx):
+    f, M, K, N = lib.FP4_MX_NVFP4, 16, 3000, 512
+    w = lib.fp4_mx_quantize(ctx, draw(K, N, "bf16", 1), f, codes=False, codes_t=True)
+    x = draw(M, K, "bf16", 2)
+    for a in (1e-20, 2.0, 1000.0):
+        amax = torch.tensor([a], device="cuda")
+        want, saved = lib.fp4_mx_quantize(ctx, x, f, amax=amax), lib.MXTensor(M, K, "cuda", f)
+        saved.amax.copy_(amax)
+        saved.struct.flags = 1
+        y, _, _ = lib.fp4_mx_linear_fwd(ctx, x, None, f, saved, w, reuse_w=True)
+        assert torch.equal(saved.codes, want.codes) and torch.equal(saved.scales, want.scales) and torch.equal(saved.amax, amax)
+        assert torch.equal(y, lib.fp4_mx_gemm(ctx, want, w, b_t=True))
