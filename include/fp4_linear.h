@@ -11,7 +11,7 @@
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - Every tensor pointer is a DEVICE pointer unless the parameter is documented as host.
- *    Tensors are dense, row-major and 16-byte aligned.  The caller owns every tensor; the
+ *    Tensors are dense, row-major and 16-byte aligned (matrices of fp4_mx_*: see there).  The caller owns every tensor; the
  *    context owns only its workspace.  After fp4_create() the library allocates no buffer; the
  *    third fp4_quantize / fp4_linear_fwd / fp4_linear_bwd with the same arguments on a context
  *    instantiates its launches as a CUDA graph that later calls replay, for which the driver takes
@@ -19,7 +19,7 @@
  *    none while the caller's stream is being captured), and profiling mode, fp4_profile_enable,
  *    creates a pair of CUDA events per kernel class and call.
  *  - Notation: A[M x K] activations, W[K x N] weights (input channels x output channels),
- *    Y[M x N] = A W.  M, K and N must be multiples of 128.
+ *    Y[M x N] = A W.  M, K and N must be multiples of 128 (fp4_mx_*: any sizes).
  *  - E2M1 codes are sign-magnitude nibbles (bit 3 sign; 0..7 -> 0, .5, 1, 1.5, 2, 3, 4, 6),
  *    two per byte with the even element in bits 3:0.  A negative zero code is never written.
  *  - Calls are asynchronous on `stream` (a cudaStream_t passed as void*).  They return 0 or
@@ -29,8 +29,8 @@
  *    streams); use one context per concurrent stream.  Host threads that call into one context
  *    take turns.
  *  - Conditions found on the device are OR-ed into the caller's device word `*status`
- *    (FP4_DEV_* bits).  When a bit is set the outputs are unspecified but every write stayed
- *    inside the caller's buffers.  Every device-side wait is bounded: a stalled pipeline
+ *    (FP4_DEV_* bits).  When a bit is set the outputs are unspecified (fp4_mx_* say more of a
+ *    non-finite input) but every write stayed inside the caller's buffers.  Every device-side wait is bounded: a stalled pipeline
  *    sets FP4_DEV_TIMEOUT and the kernel returns.
  */
 #ifndef FP4_LINEAR_H_
@@ -58,7 +58,7 @@ extern "C" {
 
 /* bits of the device status word (bit 0 is not used: the residual cannot outgrow a capacity the
  * host has accepted, see fp4_sparse_capacity) */
-#define FP4_DEV_NONFINITE        2   /* an input holds an infinity or a NaN: outputs unspecified */
+#define FP4_DEV_NONFINITE        2   /* an input holds an infinity or a NaN: outputs unspecified (fp4_mx_*: of its block) */
 #define FP4_DEV_TIMEOUT          4   /* a bounded wait inside a kernel ran out               */
 
 /* fp4_qtensor.format: how a quantised operand is stored */
@@ -456,8 +456,8 @@ int fp4_mx_gemm(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* a, const fp4_mx
  * direction that has buffers: the ones for the backward pass may be left out (serving).  `reuse`: FP4_REUSE_X /
  * FP4_REUSE_W -- that operand is there already (x or w may then be NULL).  saved_x and saved_w have the same
  * format, FP4_MX_E2M1 or FP4_MX_NVFP4, and are two tensors with an amax each, unless both are reused.  dx or dw
- * may be NULL.  `flags` of the backward: FP4_MX_ACCUMULATE_DX /
- * _DW add to what is there (a sum over consumers or micro-batches).
+ * may be NULL.  `flags` of the backward: FP4_MX_ACCUMULATE_DX / _DW add to what is there (a sum over consumers or
+ * micro-batches).  A few tokens onto a weight that is there (FP4_REUSE_W, saved_x without codes_t) are one launch.
  */
 #define FP4_REUSE_X FP4_REUSE_A
 #define FP4_MX_ACCUMULATE_DX 1
