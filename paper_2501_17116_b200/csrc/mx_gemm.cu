@@ -1190,11 +1190,11 @@ int launch_mx_linear_few(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize& x,
   *done = false;
   if (g.I > FEW_X_ROWS || x.q->codes_t) return FP4_OK;
   const FewForm few = choose_few(ctx, g);
-  if (few.cost > choose_form(ctx, &g, 1).cost) return FP4_OK;
-  // A launch and its wait against what every CTA does again.  Tokens x contraction x weight rows, us, made by the kernel / by the quantiser:
-  // 1 x 4096 x 11008 8.8 / 10.1, 4 x 11008 x 4096 9.9 / 10.9 (44 parts), 6 x 4096 x 11008 9.8 / 10.1 (48), 8 x 4096 x 11008 10.5 / 9.4 (64).
-  const int64_t per_cta = ((g.C + 255) / 256 + few.splits - 1) / few.splits;
-  if (per_cta > FEW_X_BLOCKS || g.I * per_cta > FEW_X_PARTS) return FP4_OK;
+  // A launch and its wait (1200 ns) against what every CTA does again (40 a part).  Tokens x contraction x weight rows, us, made by the kernel / by the
+  // quantiser: 1 x 4096 x 11008 8.8 / 10.1, 4 x 11008 x 4096 9.9 / 10.9 (44 parts), 6 x 4096 x 11008 9.8 / 10.1 (48), 8 x 4096 x 11008 10.5 / 9.4 (64);
+  // beside tiles, which few tokens take where the contraction is short, 8 x 1024 x 1024 4.8 / 5.5 (16), 16 x 1024 x 512 5.8 / 5.4 (32).
+  const int64_t per_cta = ((g.C + 255) / 256 + few.splits - 1) / few.splits, parts = g.I * per_cta;
+  if (per_cta > FEW_X_BLOCKS || parts > FEW_X_PARTS || few.cost + 40 * parts > choose_form(ctx, &g, 1).cost + 1200) return FP4_OK;
   // Where every CTA has to look for the amax first: 1 x 13824 x 5120 13.0 / 14.9, 1 x 4096 x 4096 7.6 / 8.5, 2 x 4096 x 11008 11.5 / 10.5.
   const bool find = nv && !(x.q->flags & FP4_MX_AMAX_GIVEN);
   if (find && g.I > 1) return FP4_OK;
