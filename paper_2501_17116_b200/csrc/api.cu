@@ -179,11 +179,11 @@ int fp4_create(fp4_ctx** out, int device, size_t workspace_bytes) {
   ok = ok && quantize_setup() == FP4_OK;
   ctx->graphs = new (std::nothrow) CallGraphs();
   ok = ok && ctx->graphs && ctx->graphs->init();
-  // counters of the quantile selection (quantisation with clamping): cleared here, once
-  ok = ok && cudaMalloc(reinterpret_cast<void**>(&ctx->occ_hist), quantize_persistent_bytes()) == cudaSuccess;
-  ok = ok && cudaMemset(ctx->occ_hist, 0, quantize_persistent_bytes()) == cudaSuccess;
-  ok = ok && cudaMalloc(reinterpret_cast<void**>(&ctx->mx_scratch), MX_SCRATCH_WORDS * sizeof(uint32_t)) == cudaSuccess;
-  ok = ok && cudaMemset(ctx->mx_scratch, 0, MX_SCRATCH_WORDS * sizeof(uint32_t)) == cudaSuccess;
+  // counters of the quantile selection (quantisation with clamping) and behind them the block-scaled operands' words: cleared here, once
+  const size_t counters = (quantize_persistent_bytes() + 255) / 256 * 256, all = counters + MX_SCRATCH_WORDS * sizeof(uint32_t);
+  ok = ok && cudaMalloc(reinterpret_cast<void**>(&ctx->occ_hist), all) == cudaSuccess;
+  ok = ok && cudaMemset(ctx->occ_hist, 0, all) == cudaSuccess;
+  if (ok) ctx->mx_scratch = ctx->occ_hist + counters / sizeof(uint32_t);
   for (auto& s : ctx->side) ok = ok && cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking) == cudaSuccess;
   for (auto& e : ctx->ev) ok = ok && cudaEventCreateWithFlags(&e, cudaEventDisableTiming) == cudaSuccess;
   ok = ok && cudaStreamCreateWithFlags(&ctx->copy_stream, cudaStreamNonBlocking) == cudaSuccess;
@@ -217,7 +217,6 @@ int fp4_destroy(fp4_ctx* ctx) {
   for (auto& e : ctx->host_step_copied)
     if (e) cudaEventDestroy(e);
   if (ctx->workspace) cudaFree(ctx->workspace);
-  if (ctx->mx_scratch) cudaFree(ctx->mx_scratch);
   if (ctx->occ_hist) cudaFree(ctx->occ_hist);      // waits for the GPU, so no graph is running below
   delete ctx->graphs;
   if (ctx->records) {

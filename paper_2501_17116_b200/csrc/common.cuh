@@ -45,7 +45,7 @@ struct fp4_ctx {
   char*    workspace;
   size_t   workspace_bytes;
   void*    encode_tiled;       // cuTensorMapEncodeTiled, fetched through the runtime
-  uint32_t* mx_scratch;        // block-scaled operands: the blocks' parts of a tensor's amax (MX_SCRATCH_WORDS, the last a ticket)
+  uint32_t* mx_scratch;        // block-scaled operands: the blocks' parts of a tensor's amax (MX_SCRATCH_WORDS, the last two tickets; behind occ_hist)
   uint32_t* occ_hist;          // quantile selection: two sets of global counters, parity, ticket
   cudaStream_t side[2];        // side streams for independent kernel chains inside one call
   cudaEvent_t  ev[10];          // fork / join events of those chains

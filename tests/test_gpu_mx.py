@@ -826,3 +826,35 @@ def test_few_tokens_with_a_given_amax(lib, ctx):
         y, _, _ = lib.fp4_mx_linear_fwd(ctx, x, None, f, saved, w, reuse_w=True)
         assert torch.equal(saved.codes, want.codes) and torch.equal(saved.scales, want.scales) and torch.equal(saved.amax, amax)
         assert torch.equal(y, lib.fp4_mx_gemm(ctx, want, w, b_t=True))
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+def test_few_tokens_captured_and_with_a_copy_that_never_comes(lib, fmt):
+    """The serving call in a graph, replayed on new tokens; and the wait that runs out in the kernel that makes the operand itself."""
+    c, f, M, K, N = lib.Context(0, 0), fmt_of(lib, fmt), 1, 2000, 640
+    w = lib.fp4_mx_quantize(c, draw(K, N, "bf16", 1), f, codes=False, codes_t=True)
+    x, y, saved = draw(M, K, "bf16", 2), torch.empty((M, N), device="cuda"), lib.MXTensor(M, K, "cuda", f)
+    call = lambda out: lib.fp4_mx_linear_fwd(c, x, None, f, saved, w, reuse_w=True, out=out)     # noqa: E731
+    call(y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(y)
+        call(y)                                              # back to back: the second one starts while the first drains
+    for seed in (3, 4):
+        x.copy_(draw(M, K, "bf16", seed))
+        graph.replay()
+        assert torch.equal(y, lib.fp4_mx_gemm(c, lib.fp4_mx_quantize(c, x, f), w, b_t=True, dtype=torch.float32))
+    torch.cuda.synchronize()
+    c.debug_set(lib.binding.FP4_DEBUG_WAIT_LIMIT_US, 1000)
+    c.debug_set(lib.binding.FP4_DEBUG_SKIP_FILL, 1)
+    call(torch.empty_like(y))
+    torch.cuda.synchronize()
+    assert c.read_status() & lib.FP4_DEV_TIMEOUT
+    c.debug_set(lib.binding.FP4_DEBUG_SKIP_FILL, -1)
+    c.debug_set(lib.binding.FP4_DEBUG_WAIT_LIMIT_US, 0)
+    c.status.zero_()
+    again = torch.empty_like(y)
+    call(again)
+    assert torch.equal(again, y) and c.read_status() == 0
+    c.close()
