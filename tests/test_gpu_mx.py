@@ -858,3 +858,33 @@ def test_few_tokens_captured_and_with_a_copy_that_never_comes(lib, fmt):
     call(again)
     assert torch.equal(again, y) and c.read_status() == 0
     c.close()
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+@pytest.mark.parametrize("M", [1, 12, 100, 700])
+def test_calls_back_to_back_keep_their_order(lib, ctx, fmt, M):
+    """A chain of calls that each read what the one before wrote and write what it read, without a wait between them (each kernel starts while the
+    one before drains): the bits of the same chain with a wait behind every call."""
+    f, K, F = fmt_of(lib, fmt), 520, 640
+    wu = lib.fp4_mx_quantize(ctx, draw(K, 2 * F, "bf16", 1, 0.0), f, True, True)
+    wd = lib.fp4_mx_quantize(ctx, draw(F, K, "bf16", 2, 0.0), f, True, True)
+    start = draw(M, K, "bf16", 3, 0.0)
+
+    def chain(pause):
+        new = lambda r, c: torch.empty((r, c), dtype=torch.bfloat16, device="cuda")            # noqa: E731
+        x, gu, h, products = start.clone(), new(M, 2 * F), new(M, F), [new(M, M) for _ in range(12)]
+        sx, sh, kept, q8 = lib.MXTensor(M, K, "cuda", f), lib.MXTensor(M, F, "cuda", f), lib.SwigluCheckpoint(M, F, "cuda"), lib.MXTensor(M, F, "cuda")
+        for product in products:
+            for call in (lambda: lib.fp4_mx_linear_fwd(ctx, x, None, f, sx, wu, reuse_w=True, out=gu),
+                         lambda: lib.fp4_mx_swiglu_fwd(ctx, gu[:, :F], gu[:, F:], out=h, checkpoint=kept),
+                         lambda: lib.fp4_mx_linear_fwd(ctx, h, None, f, sh, wd, reuse_w=True, out=x),
+                         lambda: lib.fp4_mx_swiglu_bwd(ctx, h, kept, dgate=gu[:, :F], dup=gu[:, F:], quantized=q8),
+                         lambda: lib.fp4_mx_dequantize(ctx, q8, out=h),
+                         lambda: lib.fp4_mx_gemm(ctx, sx, sx, out=product),
+                         lambda: lib.fp4_mx_dequantize(ctx, sx, out=x)):
+                call()
+                if pause:
+                    torch.cuda.synchronize()
+        return [x, gu, h, q8.codes, sh.codes] + products
+
+    assert all(torch.equal(a, b) for a, b in zip(chain(False), chain(True)))
