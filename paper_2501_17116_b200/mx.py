@@ -1,4 +1,5 @@
-"""Binding of the block-scaled operands (fp4_mx_* of include/fp4_linear.h): argument marshalling only.
+"""Binding of the block-scaled operands (fp4_mx_* of include/fp4_linear.h): argument marshalling only, the tensors' part of it in
+csrc/mx_call.cpp.
 
 Tensors may have any row stride (their last dimension is contiguous); the calls run on the context's device,
 on the stream that is current there.
@@ -6,7 +7,6 @@ on the stream that is current there.
 from __future__ import annotations
 
 import ctypes as C
-from struct import Struct
 
 import torch
 
@@ -28,14 +28,6 @@ FP4_REUSE_W = 1
 FP4_REUSE_X = 2
 
 
-class _Dtypes(dict):
-    def __missing__(self, dtype):
-        raise AssertionError(f"{dtype}: a matrix is of torch.bfloat16, torch.float16 or torch.float32")
-
-
-_DTYPES = _Dtypes({torch.bfloat16: FP4_DTYPE_BF16, torch.float16: FP4_DTYPE_FP16, torch.float32: FP4_DTYPE_FP32})
-
-
 class fp4_mx_matrix(C.Structure):
     _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
@@ -46,10 +38,18 @@ class fp4_mx_tensor(C.Structure):
                 ("flags", C.c_int32)]
 
 
+ENTRIES = ("quantize", "dequantize", "gemm", "linear_fwd", "linear_bwd", "swiglu_fwd", "swiglu_bwd")
+QUANTIZE, DEQUANTIZE, GEMM, LINEAR_FWD, LINEAR_BWD, SWIGLU_FWD, SWIGLU_BWD = range(7)
+
+
 def declare(lib: C.CDLL):
-    """Prototypes of the fp4_mx_* functions."""
+    """Prototypes of the fp4_mx_* functions, and the addresses that _mx_call takes."""
+    global _call
+    if _call is None:
+        from . import _mx_call
+        _call = _mx_call
     vp, i64, i32 = C.c_void_p, C.c_int64, C.c_int
-    mat, ten = vp, C.POINTER(fp4_mx_tensor)          # (an fp4_mx_matrix by reference, or its bytes)
+    mat, ten = C.POINTER(fp4_mx_matrix), C.POINTER(fp4_mx_tensor)
     lib.fp4_mx_pitch.argtypes, lib.fp4_mx_pitch.restype = [i64, i32], i64
     lib.fp4_mx_scale_bytes.argtypes, lib.fp4_mx_scale_bytes.restype = [i64, i64, i32], i64
     lib.fp4_mx_workspace_bytes.argtypes, lib.fp4_mx_workspace_bytes.restype = [i64, i64, i64], C.c_size_t
@@ -60,24 +60,20 @@ def declare(lib: C.CDLL):
                        ("swiglu_bwd", [mat, ten, ten, i64, i64, mat, mat, mat, ten, vp])):
         f = getattr(lib, "fp4_mx_" + name)
         f.argtypes, f.restype = [vp, vp] + args, i32
+    lib.mx_entries = tuple(C.cast(getattr(lib, "fp4_mx_" + name), vp).value for name in ENTRIES)
 
 
 _stream_of = torch._C._cuda_getCurrentRawStream
-_pack = Struct("@Pqii").pack               # the bytes of an fp4_mx_matrix: a ctypes structure takes three times as long to make
-assert Struct("@Pqii").size == C.sizeof(fp4_mx_matrix)
+_call = None                               # the module _mx_call, once a library is loaded
 
 
-def _matrix(ctx: Context, t):
-    """Structure of a matrix (None: of none)."""
-    if t is None:
-        return None
-    rows, cols = t.stride()
-    assert t.get_device() == ctx.device and (cols == 1 or t.shape[1] <= 1)
-    return _pack(t.data_ptr(), rows, _DTYPES[t.dtype], 0)
+def _head(ctx: Context, entry: int):
+    """What every call begins with."""
+    return ctx.lib.mx_entries[entry], ctx.handle.value, _stream_of(ctx.device), ctx.status.data_ptr(), ctx.device
 
 
 def _tensor(ctx: Context, q):
-    """Reference to an operand's structure (None: of none)."""
+    """Address of an operand's structure (None: of none)."""
     if q is None:
         return None
     assert q.device == ctx.device, f"an operand on device {q.device}, the context on device {ctx.device}"
@@ -104,7 +100,7 @@ class MXTensor:
         where = lambda t: None if t is None else (t.data_ptr() or 16)                         # noqa: E731
         self.struct = fp4_mx_tensor(rows, cols, where(self.codes), where(self.scales), where(self.codes_t), where(self.scales_t),
                                     _ptr(self.amax), fmt, 0)
-        self.ref = C.byref(self.struct)
+        self.ref = C.addressof(self.struct)
         self.device = (self.codes if codes else self.codes_t).get_device() if codes or codes_t else -1
 
 
@@ -122,12 +118,11 @@ def fp4_mx_quantize(ctx: Context, x: torch.Tensor, fmt: int = FP4_MX_E2M1, codes
     device) is taken for the tensor's largest magnitude instead of looking for it."""
     if out is None:
         out = MXTensor(*x.shape, x.device, fmt, codes, codes_t)
-    assert x.shape == (out.rows, out.cols)
     given = amax is not None and out.amax is not None
     if given:
         out.amax.copy_(amax.reshape(1))
         out.struct.flags = FP4_MX_AMAX_GIVEN
-    rc = ctx.lib.fp4_mx_quantize(ctx.handle, _stream_of(ctx.device), _matrix(ctx, x), _tensor(ctx, out), ctx.status.data_ptr())
+    rc = _call.quantize(*_head(ctx, QUANTIZE), x, _tensor(ctx, out))
     if given:
         out.struct.flags = 0
     _check(rc)
@@ -137,25 +132,20 @@ def fp4_mx_quantize(ctx: Context, x: torch.Tensor, fmt: int = FP4_MX_E2M1, codes
 def fp4_mx_dequantize(ctx: Context, q: MXTensor, transposed: bool = False, dtype=torch.bfloat16,
                       out: torch.Tensor | None = None) -> torch.Tensor:
     """The values of `q.codes` [rows x cols], or of `q.codes_t` [cols x rows]."""
-    shape = (q.cols, q.rows) if transposed else (q.rows, q.cols)
     if out is None:
-        out = _new(ctx, *shape, dtype)
-    assert out.shape == shape
-    _check(ctx.lib.fp4_mx_dequantize(ctx.handle, _stream_of(ctx.device), _tensor(ctx, q), int(transposed), _matrix(ctx, out),
-                                     ctx.status.data_ptr()))
+        out = _new(ctx, *((q.cols, q.rows) if transposed else (q.rows, q.cols)), dtype)
+    _check(_call.dequantize(*_head(ctx, DEQUANTIZE), _tensor(ctx, q), int(transposed), out))
     return out
 
 
 def fp4_mx_gemm(ctx: Context, a: MXTensor, b: MXTensor, a_t: bool = False, b_t: bool = False, dtype=torch.bfloat16,
                 out: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
     """out (+)= a b^T over the rows' blocks of each operand: of `codes`, or with a_t / b_t of `codes_t`."""
-    shape = (a.cols if a_t else a.rows, b.cols if b_t else b.rows)
     if out is None:
         assert not accumulate
-        out = _new(ctx, *shape, dtype)
-    assert out.shape == shape
+        out = _new(ctx, a.cols if a_t else a.rows, b.cols if b_t else b.rows, dtype)
     flags = (FP4_MX_A_T if a_t else 0) | (FP4_MX_B_T if b_t else 0) | (FP4_MX_ACCUMULATE if accumulate else 0)
-    _check(ctx.lib.fp4_mx_gemm(ctx.handle, _stream_of(ctx.device), _tensor(ctx, a), _tensor(ctx, b), flags, _matrix(ctx, out), ctx.status.data_ptr()))
+    _check(_call.gemm(*_head(ctx, GEMM), _tensor(ctx, a), _tensor(ctx, b), flags, out))
     return out
 
 
@@ -177,11 +167,9 @@ def fp4_mx_linear_fwd(ctx: Context, X: torch.Tensor | None, W: torch.Tensor | No
         assert (saved_w.rows, saved_w.cols) == (K, N)
     if out is None:
         out = _new(ctx, M, N, dtype or (X.dtype if X is not None else torch.bfloat16))
-    assert out.shape == (M, N)
     reuse = (FP4_REUSE_X if reuse_x else 0) | (FP4_REUSE_W if reuse_w else 0)
-    _check(ctx.lib.fp4_mx_linear_fwd(ctx.handle, _stream_of(ctx.device), None if reuse_x else _matrix(ctx, X),
-                                     None if reuse_w else _matrix(ctx, W), M, K, N, reuse, _matrix(ctx, out),
-                                     _tensor(ctx, saved_x), _tensor(ctx, saved_w), ctx.status.data_ptr()))
+    _check(_call.linear_fwd(*_head(ctx, LINEAR_FWD), None if reuse_x else X, None if reuse_w else W, M, K, N, reuse, out, _tensor(ctx, saved_x),
+                            _tensor(ctx, saved_w)))
     return out, saved_x, saved_w
 
 
@@ -197,10 +185,8 @@ def fp4_mx_linear_bwd(ctx: Context, dY: torch.Tensor, saved_x: MXTensor, saved_w
     if dW is None and want_dw:
         assert not accumulate_dw
         dW = _new(ctx, K, N, dtype or dY.dtype)
-    assert (dX is None or dX.shape == (M, K)) and (dW is None or dW.shape == (K, N))
     flags = (FP4_MX_ACCUMULATE_DX if accumulate_dx else 0) | (FP4_MX_ACCUMULATE_DW if accumulate_dw else 0)
-    _check(ctx.lib.fp4_mx_linear_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dY), _tensor(ctx, saved_x), _tensor(ctx, saved_w), M, K, N,
-                                     flags, _matrix(ctx, dX), _matrix(ctx, dW), ctx.status.data_ptr()))
+    _check(_call.linear_bwd(*_head(ctx, LINEAR_BWD), dY, _tensor(ctx, saved_x), _tensor(ctx, saved_w), M, K, N, flags, dX, dW))
     return dX, dW
 
 
@@ -210,7 +196,6 @@ def fp4_mx_swiglu_fwd(ctx: Context, gate: torch.Tensor, up: torch.Tensor, out: t
     shape = rows, cols = gate.shape
     if out is None and want_h:
         out = _new(ctx, rows, cols, gate.dtype)
-    assert up.shape == shape and (out is None or out.shape == shape)
     g = u = q = None
     if checkpoint is not None:
         assert (checkpoint.gate.rows, checkpoint.gate.cols) == shape
@@ -218,8 +203,7 @@ def fp4_mx_swiglu_fwd(ctx: Context, gate: torch.Tensor, up: torch.Tensor, out: t
     if quantized is not None:
         assert (quantized.rows, quantized.cols) == shape
         q = _tensor(ctx, quantized)
-    _check(ctx.lib.fp4_mx_swiglu_fwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, gate), _matrix(ctx, up), rows, cols,
-                                     _matrix(ctx, out), g, u, q, ctx.status.data_ptr()))
+    _check(_call.swiglu_fwd(*_head(ctx, SWIGLU_FWD), gate, up, rows, cols, out, g, u, q))
     return out, checkpoint, quantized
 
 
@@ -229,12 +213,9 @@ def fp4_mx_swiglu_bwd(ctx: Context, dh: torch.Tensor, checkpoint: SwigluCheckpoi
     shape = rows, cols = dh.shape
     dgate = _new(ctx, rows, cols, dh.dtype) if dgate is None else dgate
     dup = _new(ctx, rows, cols, dh.dtype) if dup is None else dup
-    assert dgate.shape == shape and dup.shape == shape and (h is None or h.shape == shape)
     q = None
     if quantized is not None:
         assert (quantized.rows, quantized.cols) == shape
         q = _tensor(ctx, quantized)
-    _check(ctx.lib.fp4_mx_swiglu_bwd(ctx.handle, _stream_of(ctx.device), _matrix(ctx, dh), _tensor(ctx, checkpoint.gate),
-                                     _tensor(ctx, checkpoint.up), rows, cols,
-                                     _matrix(ctx, dgate), _matrix(ctx, dup), _matrix(ctx, h), q, ctx.status.data_ptr()))
+    _check(_call.swiglu_bwd(*_head(ctx, SWIGLU_BWD), dh, _tensor(ctx, checkpoint.gate), _tensor(ctx, checkpoint.up), rows, cols, dgate, dup, h, q))
     return dgate, dup

@@ -178,3 +178,20 @@ def test_binding_refuses_an_operand_of_another_device(lib):
         fp4.mx._tensor(SimpleNamespace(device=0), q)
     assert fp4.mx._tensor(SimpleNamespace(device=-1), q) is q.ref                               # (torch's number for the CPU)
     assert fp4.mx._tensor(SimpleNamespace(device=0), None) is None
+
+
+def test_binding_refuses_what_is_no_matrix_of_the_call(lib):
+    """Each is refused ahead of the call (whose address here is of no function)."""
+    call, head = fp4.mx._call, (16, None, 0, P, 0)
+    q = ten(4, 64)
+    at = C.addressof(q)
+    for bad in (torch.zeros(4, 64), torch.zeros(4, 63), torch.zeros(64), torch.zeros(2, 2, 64), "a tensor", 7,
+                torch.zeros(4, 64, device="meta"), torch.zeros(4, 64).to_sparse()):
+        with pytest.raises(AssertionError):
+            call.quantize(*head, bad, at)
+    with pytest.raises(TypeError):
+        call.quantize(*head, None)
+    with pytest.raises(TypeError):
+        call.gemm(*head, at, at, "flags", None)
+    with pytest.raises(ValueError):
+        call.quantize(None, None, 0, P, 0, None, at)
