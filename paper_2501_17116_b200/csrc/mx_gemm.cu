@@ -151,17 +151,18 @@ struct OutArgs {
   bool accumulate;
   bool bulk;                   // rows begin and end on 16-byte boundaries: bulk stores
 };
-// The tensors' powers of two (1 without them).
+// The tensors' powers of two (none without them).  Their product 2^k, k from -200 to 236, is applied in two halves of one sign: the first step never
+// leaves fp32's range where the result stays inside (2^ka, then 2^kb does: values near 1e35 times weights of 0.02 came out infinite), and, the sums
+// being multiples of 2^-20, never rounds.
 struct Powers {
   const uint32_t *a, *b;
 };
+__device__ __forceinline__ float2 tensor_scales(uint32_t amax_a, uint32_t amax_b) {
+  const int k = mx_tensor_exponent(amax_a) + mx_tensor_exponent(amax_b);
+  return make_float2(mx_codes::pow2_int(k / 2), mx_codes::pow2_int(k - k / 2));
+}
 __device__ __forceinline__ float2 tensor_scales(const Powers& p) {
-  float2 s = make_float2(1.0f, 1.0f);
-  if (p.a) {
-    s.x = __uint_as_float(uint32_t(mx_tensor_exponent(__ldg(p.a)) + 127) << 23);
-    s.y = __uint_as_float(uint32_t(mx_tensor_exponent(__ldg(p.b)) + 127) << 23);
-  }
-  return s;
+  return p.a ? tensor_scales(__ldg(p.a), __ldg(p.b)) : make_float2(1.0f, 1.0f);
 }
 
 // 32 rows x 32 columns (the last ones: fewer) of a warp, row `lane` in y.  Ways out:
@@ -928,13 +929,7 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (args.splits > 1) cluster_sync_all();
-  float2 scales = make_float2(1.0f, 1.0f);
-  if (MAKE && FMT == FP4_MX_NVFP4) {
-    scales.x = mx_codes::pow2_int(mx_tensor_exponent(*s_amax));
-    scales.y = mx_codes::pow2_int(mx_tensor_exponent(__ldg(args.powers.b)));
-  } else {
-    scales = tensor_scales(args.powers);
-  }
+  const float2 scales = MAKE && FMT == FP4_MX_NVFP4 ? tensor_scales(*s_amax, __ldg(args.powers.b)) : tensor_scales(args.powers);
   // four neighbouring columns of a token at a time, and four such fours on their way together
   constexpr int AT_ONCE = 4;
   const int step = args.splits * int(blockDim.x), n = args.out.I * (BM / 4);
