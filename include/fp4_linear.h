@@ -365,7 +365,8 @@ int fp4_quantile_thresholds_static(void* stream, const void* x_bf16, int64_t row
  *                 [-127, 127] with amax <= 6 * 2^e, amax the block's largest magnitude (a block of zeros:
  *                 -127); code = E2M1(x * 2^-e).  ("MXFP4".)
  *   FP4_MX_NVFP4  E2M1 nibbles, blocks of 16, an E4M3 scale s each and a scale g of the whole tensor: g is
- *                 the least power of two, 2^-100 at least, with the tensor's amax <= 6 * 448 * g;
+ *                 the least power of two, 2^-100 at least, with the tensor's amax (its largest finite
+ *                 magnitude) <= 6 * 448 * g;
  *                 s = E4M3(amax / g / 6), code = E2M1(x / g / s), 0 where s is 0.  The tensor's amax is kept
  *                 (`amax`), g follows from it.
  *   FP4_MX_E4M3   E4M3 bytes, blocks of 32, scale 2^e with amax <= 448 * 2^e: the 8-bit form in which
@@ -412,10 +413,10 @@ typedef struct fp4_mx_tensor {
   uint8_t* scales;     /* [fp4_mx_scale_bytes(rows, cols)]                                           */
   uint8_t* codes_t;    /* [cols x fp4_mx_pitch(rows)]                                                */
   uint8_t* scales_t;   /* [fp4_mx_scale_bytes(cols, rows)]                                           */
-  float*   amax;       /* [1] FP4_MX_NVFP4: largest magnitude of the tensor; else NULL               */
+  float*   amax;       /* [1] FP4_MX_NVFP4: largest finite magnitude of the tensor; else NULL        */
   int32_t  format;     /* FP4_MX_*, set by the caller                                                */
-  int32_t  flags;      /* FP4_MX_AMAX_GIVEN: `amax` holds a value already (of earlier data, say): it is
-                          used and one pass over the tensor is saved; what exceeds it may saturate       */
+  int32_t  flags;      /* FP4_MX_AMAX_GIVEN: `amax` holds a value already (of earlier data, say), finite:
+                          it is used and one pass over the tensor is saved; what exceeds it may saturate */
 } fp4_mx_tensor;
 #define FP4_MX_AMAX_GIVEN 1
 

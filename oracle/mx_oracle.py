@@ -7,7 +7,7 @@ and without a table or helper in common with it.  NumPy, float64; written from t
   (bias 7, subnormals, no infinity, 448 the largest); nearest value, a tie to the even code;
 * "mxfp4": blocks of 32, scale 2^e, e the least integer in [-127, 127] with amax <= 6 * 2^e; "mxfp8": E4M3
   elements, 448 in place of 6; "nvfp4": blocks of 16, g = 2^k with k >= -100 the least integer with
-  amax(tensor) <= 2688 * 2^k, s = E4M3(amax(block) / g / 6), elements E2M1(x / g / s), 0 where s is 0.
+  amax(tensor) <= 2688 * 2^k (infinities and NaNs left out), s = E4M3(amax(block) / g / 6), elements E2M1(x / g / s), 0 where s is 0.
   The two quotients are float32 numbers (RN32).
 """
 from __future__ import annotations
@@ -68,10 +68,9 @@ def quantize(x: np.ndarray, fmt: str, amax: float | None = None) -> Quantized:
     finite = np.isfinite(b).all(axis=2)
     b = np.where(finite[:, :, None], b, 0.0)
     top = np.abs(b).max(axis=2) if b.size else np.zeros((rows, nb))
-    tensor = float(np.abs(x).max()) if amax is None and x.size else float(amax or 0.0)
+    tensor = float(np.abs(x[np.isfinite(x)]).max(initial=0.0)) if amax is None else float(amax)
     if fmt == "nvfp4":
-        # (an infinity or a NaN in the tensor counts as the largest exponent)
-        k = int(least_exponent(np.array([tensor]), 2688.0, -100)[0]) if np.isfinite(tensor) else (118 if np.isnan(tensor) else 117)
+        k = int(least_exponent(np.array([tensor]), 2688.0, -100)[0])
         s_code = nearest_code(rn32(np.ldexp(top, -k) / 6.0), E4M3)
         s = E4M3[s_code]
         with np.errstate(divide="ignore", invalid="ignore"):

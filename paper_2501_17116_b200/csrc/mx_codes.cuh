@@ -72,6 +72,13 @@ template <> struct TypeOf<float> {
   }
   __device__ static float value(uint32_t bits) { return __uint_as_float(bits); }
 };
+// The larger of a pattern and the finite magnitudes in a word (two of 16 bits, or one).
+template <class T>
+__device__ __forceinline__ uint32_t most_finite(uint32_t m, uint32_t w) {
+  constexpr uint32_t MAGNITUDE = sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFFu;
+  const uint32_t lo = w & MAGNITUDE, hi = sizeof(T) == 4 ? 0u : (w >> 16) & MAGNITUDE;
+  return max(m, max(lo < TypeOf<T>::INF ? lo : 0u, hi < TypeOf<T>::INF ? hi : 0u));
+}
 // -------------------------------------------------------------------------------- codes ----
 __device__ __forceinline__ uint32_t e2m1_word(const f32x2 (&v)[4]) {      // eight elements, the first in the low nibble
   float f[8];

@@ -720,7 +720,7 @@ __device__ __forceinline__ uint32_t amax_of_eight(const uint32_t (&w)[2 * sizeof
   if constexpr (sizeof(T) == 4) return m & 0x7FFFFFFFu;
   else return max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
 }
-// Largest magnitude of the token, as a pattern of fp32, in every thread of warps 2 and up (`s_max`: a word for each).
+// Largest finite magnitude of the token, as a pattern of fp32, in every thread of warps 2 and up (`s_max`: a word for each).
 template <class T>
 __device__ __forceinline__ uint32_t few_amax(const FewX& x, uint32_t* s_max) {
   const int threads = int(blockDim.x) - 64, t = int(threadIdx.x) - 64;
@@ -732,6 +732,16 @@ __device__ __forceinline__ uint32_t few_amax(const FewX& x, uint32_t* s_max) {
     for (int i = 0; i < 4; ++i) load_eight<T>(x, 0, (c + i * threads < pieces ? c + i * threads : c) * 8, w[i]);
 #pragma unroll
     for (int i = 0; i < 4; ++i) m = max(m, amax_of_eight<T>(w[i]));
+  }
+  if (m >= mx_codes::TypeOf<T>::INF) {                       // (the thread met something that is not finite: once more, without it)
+    m = 0;
+#pragma unroll 1
+    for (int64_t c = t; c < pieces; c += threads) {
+      uint32_t w[2 * sizeof(T)];
+      load_eight<T>(x, 0, c * 8, w);
+#pragma unroll
+      for (int i = 0; i < 2 * int(sizeof(T)); ++i) m = mx_codes::most_finite<T>(m, w[i]);
+    }
   }
   m = __reduce_max_sync(0xFFFFFFFFu, m);
   if ((threadIdx.x & 31) == 0) s_max[(threadIdx.x >> 5) - 2] = m;

@@ -436,7 +436,8 @@ __device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* s_max) {
 }
 
 // ------------------------------------------------------------------ a tensor's amax (NVFP4) ---
-// Largest magnitude of a matrix as a pattern of fp32, for the block that calls.  Warps `warp`, `warp + warps`, ... take pieces of a row in
+// Largest finite magnitude of a matrix as a pattern of fp32, for the block that calls.  (An infinity or a NaN makes its own block's scale a NaN; as the
+// tensor's amax it would make every other block's scale, and all codes with it, 0.)  Warps `warp`, `warp + warps`, ... take pieces of a row in
 // 16-byte loads, AT_ONCE a lane on their way together; what lies outside of whole aligned pieces goes element by element.  (Maxima of
 // integers: their order does not matter.)
 struct AmaxArgs {
@@ -446,8 +447,9 @@ struct AmaxArgs {
   uint32_t* amax;              // not null: the block that ends last joins the parts here (`ticket`, 0 between calls, tells it)
   uint32_t* ticket;
 };
-template <class T>
-__device__ __forceinline__ uint32_t amax_of(const AmaxArgs& a, int64_t warp, int64_t warps, uint32_t* s_max) {
+// The thread's part of it, as a pattern of T; FINITE: of what is finite alone, which costs instructions.
+template <class T, bool FINITE>
+__device__ __forceinline__ uint32_t thread_amax(const AmaxArgs& a, int64_t warp, int64_t warps) {
   constexpr int E = int(sizeof(T)), AT_ONCE = 8;
   constexpr int64_t PIECE = 32 * AT_ONCE * 16;                               // bytes
   const int lane = threadIdx.x & 31;
@@ -456,6 +458,7 @@ __device__ __forceinline__ uint32_t amax_of(const AmaxArgs& a, int64_t warp, int
   };
   uint32_t m = 0;
   const int64_t pieces = (a.cols * E + PIECE - 1) / PIECE;
+#pragma unroll 1
   for (int64_t row = warp / pieces, piece = warp % pieces; row < a.rows;) {
     const uintptr_t begin = reinterpret_cast<uintptr_t>(a.x) + uintptr_t(row * a.ld * E), end = begin + uintptr_t(a.cols * E);
     uintptr_t body = (begin + 15) & ~uintptr_t(15), tail = end & ~uintptr_t(15);
@@ -466,21 +469,33 @@ __device__ __forceinline__ uint32_t amax_of(const AmaxArgs& a, int64_t warp, int
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i)
       q[i] = p + 512 * i < tail ? __ldg(reinterpret_cast<const uint4*>(p + 512 * i)) : make_uint4(0, 0, 0, 0);
+    const auto take = [&](uint32_t w) { m = FINITE ? most_finite<T>(m, w) : TypeOf<T>::most(m, w); };
     if (piece == 0) {                                      // up to 16 / E - 1 elements at either end
-      if (begin + lane * E < body) m = TypeOf<T>::most(m, element(begin + lane * E));
-      if (tail + lane * E < end) m = TypeOf<T>::most(m, element(tail + lane * E));
+      if (begin + lane * E < body) take(element(begin + lane * E));
+      if (tail + lane * E < end) take(element(tail + lane * E));
     }
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i)
-      m = TypeOf<T>::most(m, TypeOf<T>::most(TypeOf<T>::most(q[i].x, q[i].y), TypeOf<T>::most(q[i].z, q[i].w)));
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (FINITE) {
+        take(q[i].x); take(q[i].y); take(q[i].z); take(q[i].w);
+      } else {
+        take(TypeOf<T>::most(TypeOf<T>::most(q[i].x, q[i].y), TypeOf<T>::most(q[i].z, q[i].w)));
+      }
+    }
     piece += warps;
     if (piece >= pieces) {
       row += piece / pieces;
       piece %= pieces;
     }
   }
-  if constexpr (E == 2) m = max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
-  else m &= 0x7FFFFFFFu;
+  if (FINITE) return m;
+  if constexpr (E == 2) return max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+  else return m & 0x7FFFFFFFu;
+}
+template <class T>
+__device__ __forceinline__ uint32_t amax_of(const AmaxArgs& a, int64_t warp, int64_t warps, uint32_t* s_max) {
+  uint32_t m = thread_amax<T, false>(a, warp, warps);
+  if (m >= TypeOf<T>::INF) m = thread_amax<T, true>(a, warp, warps);         // (it met something that is not: once more)
   return block_max(__float_as_uint(TypeOf<T>::value(m)), s_max);
 }
 // One matrix or two in a launch: the first has the first `blocks` blocks.

@@ -1,0 +1,49 @@
+"""CPU-only checks of the block-scaled calls' binding: what a refused call leaves behind, and the module that the calls go through."""
+import ctypes as C
+import os
+import subprocess
+import sys
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+import paper_2501_17116_b200 as fp4
+from paper_2501_17116_b200 import build as fp4_build
+from paper_2501_17116_b200 import mx
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    fp4_build.build()
+    return fp4.load_library()
+
+
+@pytest.fixture
+def ctx(lib, monkeypatch):
+    """A context by its outside, on torch's number for the CPU: calls reach the checks of their matrices and end there."""
+    monkeypatch.setattr(mx, "_stream_of", lambda device: 0)
+    return SimpleNamespace(lib=lib, handle=C.c_void_p(0x10000), device=-1, status=torch.zeros(1, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("flags", [0, mx.FP4_MX_AMAX_GIVEN])
+@pytest.mark.parametrize("bad", [torch.zeros(4, 63), torch.zeros(5, 64), torch.zeros(4, 64, dtype=torch.float64), torch.zeros(64, 4).t(), torch.zeros(4, 64)])
+def test_a_refused_quantisation_leaves_the_operand_as_it_was(ctx, bad, flags):
+    """Shape, type, stride and device of the matrix: the call ends with an exception, and a later one finds neither flag nor amax of it."""
+    q = fp4.MXTensor(4, 64, "cpu", fp4.FP4_MX_NVFP4)
+    q.amax.fill_(3.0)
+    q.struct.flags = flags
+    before = bytes(q.struct)
+    with pytest.raises(AssertionError):
+        fp4.fp4_mx_quantize(ctx, bad, fp4.FP4_MX_NVFP4, out=q, amax=torch.tensor([0.25]))
+    assert bytes(q.struct) == before and float(q.amax) == 3.0
+
+
+def test_an_operand_of_another_device_is_refused_ahead_of_its_amax(ctx):
+    q = fp4.MXTensor(4, 64, "cpu", fp4.FP4_MX_NVFP4)
+    ctx.device = 0
+    with pytest.raises(AssertionError, match="device"):
+        fp4.fp4_mx_quantize(ctx, torch.zeros(4, 64), fp4.FP4_MX_NVFP4, out=q, amax=torch.tensor([0.25]))
+    assert q.struct.flags == 0 and float(q.amax) == 0.0

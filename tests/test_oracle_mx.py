@@ -89,3 +89,16 @@ def test_swiglu_gradient_against_differences():
 def test_e4m3_grid_is_the_other_oracles():
     codes = np.arange(0x7F, dtype=np.uint8)
     assert np.array_equal(F.e4m3_decode(codes) if hasattr(F, "e4m3_decode") else O.E4M3, O.E4M3)
+
+
+def test_the_tensors_scale_leaves_out_what_is_not_finite():
+    """Blocks of 16: the blocks without an infinity or a NaN are what they are with zeros in its place."""
+    x = np.random.default_rng(4).standard_normal((5, 64))
+    bad, zeros = x.copy(), x.copy()
+    for p, v in (((0, 3), np.inf), ((2, 40), np.nan), ((4, 63), -np.inf)):
+        bad[p], zeros[p] = v, 0.0
+    q, without = O.quantize(bad, "nvfp4"), O.quantize(zeros, "nvfp4")
+    nan = np.isnan(q.values)
+    assert q.amax == without.amax == np.abs(zeros).max() and nan.sum() == 3 * 16 and (q.codes[nan] == 0).all()
+    assert np.array_equal(q.codes[~nan], without.codes[~nan]) and np.array_equal(q.values[~nan], without.values[~nan]) and (q.codes[~nan] != 0).any()
+    assert O.quantize(np.full((1, 16), np.nan), "nvfp4").amax == 0.0
