@@ -114,18 +114,20 @@ class SwigluCheckpoint:
 
 def fp4_mx_quantize(ctx: Context, x: torch.Tensor, fmt: int = FP4_MX_E2M1, codes: bool = True, codes_t: bool = False,
                     out: MXTensor | None = None, amax: torch.Tensor | None = None) -> MXTensor:
-    """`x` in blocks along its columns (`codes`) and / or its rows (`codes_t`).  `amax` (FP4_MX_NVFP4; one float on the
-    device) is taken for the tensor's largest magnitude instead of looking for it."""
+    """`x` in blocks along its columns (`codes`) and / or its rows (`codes_t`).  `amax` (FP4_MX_NVFP4, the other formats have no
+    use for it; one finite float) is taken for the tensor's largest magnitude instead of looking for it."""
     if out is None:
         out = MXTensor(*x.shape, x.device, fmt, codes, codes_t)
+    at = _tensor(ctx, out)
     given = amax is not None and out.amax is not None
     if given:
-        out.amax.copy_(amax.reshape(1))
-        out.struct.flags = FP4_MX_AMAX_GIVEN
-    rc = _call.quantize(*_head(ctx, QUANTIZE), x, _tensor(ctx, out))
+        # (in a structure of the call's own: a call that is refused leaves the operand, its amax and its flags as they were)
+        amax = amax.detach().to(out.amax.device, torch.float32).reshape(1)
+        struct = fp4_mx_tensor.from_buffer_copy(out.struct)
+        struct.amax, struct.flags, at = amax.data_ptr(), struct.flags | FP4_MX_AMAX_GIVEN, C.addressof(struct)
+    _check(_call.quantize(*_head(ctx, QUANTIZE), x, at))
     if given:
-        out.struct.flags = 0
-    _check(rc)
+        out.amax.copy_(amax)
     return out
 
 
