@@ -459,7 +459,7 @@ int fp4_mx_gemm(fp4_ctx* ctx, void* stream, const fp4_mx_tensor* a, const fp4_mx
  * direction that has buffers: the ones for the backward pass may be left out (serving).  `reuse`: FP4_REUSE_X /
  * FP4_REUSE_W -- that operand is there already (x or w may then be NULL).  saved_x and saved_w have the same
  * format, FP4_MX_E2M1 or FP4_MX_NVFP4, and are two tensors with an amax each, unless both are reused.  dx or dw
- * may be NULL.  `flags` of the backward: FP4_MX_ACCUMULATE_DX / _DW add to what is there (a sum over consumers or
+ * may be NULL, and so may the operand that only it reads (saved_w for dx, saved_x for dw).  `flags` of the backward: FP4_MX_ACCUMULATE_DX / _DW add to what is there (a sum over consumers or
  * micro-batches).  A few tokens onto a weight that is there (FP4_REUSE_W, saved_x without codes_t) are one launch.
  */
 #define FP4_REUSE_X FP4_REUSE_A

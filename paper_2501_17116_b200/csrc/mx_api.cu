@@ -254,10 +254,11 @@ int fp4_mx_linear_fwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* x, const 
 
 int fp4_mx_linear_bwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* dy, const fp4_mx_tensor* saved_x, const fp4_mx_tensor* saved_w,
                       int64_t M, int64_t K, int64_t N, int flags, const fp4_mx_matrix* dx, const fp4_mx_matrix* dw, int32_t* status) {
-  if (!ctx || !dy || !saved_x || !saved_w || !status) return FP4_ERR_NULL;
+  if (!ctx || !dy || !status) return FP4_ERR_NULL;
   std::lock_guard<std::mutex> turn(ctx->mutex);
   if (flags & ~(FP4_MX_ACCUMULATE_DX | FP4_MX_ACCUMULATE_DW)) return FP4_ERR_ARG;
   const bool want_dx = wanted(dx), want_dw = wanted(dw);
+  if ((want_dw && !saved_x) || (want_dx && !saved_w)) return FP4_ERR_NULL;
   int rc = check_sizes(M, 2 * K);
   if (rc == FP4_OK) rc = check_sizes(K, 2 * N);
   if (rc == FP4_OK) rc = check_sizes(M, N);

@@ -175,10 +175,10 @@ def fp4_mx_linear_fwd(ctx: Context, X: torch.Tensor | None, W: torch.Tensor | No
     return out, saved_x, saved_w
 
 
-def fp4_mx_linear_bwd(ctx: Context, dY: torch.Tensor, saved_x: MXTensor, saved_w: MXTensor, dtype=None,
+def fp4_mx_linear_bwd(ctx: Context, dY: torch.Tensor, saved_x: MXTensor | None, saved_w: MXTensor | None, dtype=None,
                       dX: torch.Tensor | None = None, dW: torch.Tensor | None = None, want_dx: bool = True,
                       want_dw: bool = True, accumulate_dx: bool = False, accumulate_dw: bool = False):
-    """dX = Q(dY) Q(W)^T and dW = Q(X)^T Q(dY)."""
+    """dX = Q(dY) Q(W)^T and dW = Q(X)^T Q(dY).  `saved_x` may be None where dW is not wanted, `saved_w` where dX is not."""
     M, N = dY.shape
     K = saved_x.cols if want_dw or dW is not None else saved_w.rows
     if dX is None and want_dx:

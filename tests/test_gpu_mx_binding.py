@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_mx import check_quantized, draw
+from test_gpu_mx import check_quantized, draw, fmt_of
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +60,17 @@ def test_a_given_amax_in_a_captured_call(lib, ctx):
         graph.replay()
         torch.cuda.synchronize()
         check_quantized(q, x, "nvfp4", amax=a)
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+def test_a_backward_pass_with_the_operand_it_reads(lib, ctx, fmt):
+    f, M, K, N = fmt_of(lib, fmt), 70, 200, 130
+    x, w, dy = draw(M, K, "bf16", 7), draw(K, N, "bf16", 8), draw(M, N, "bf16", 9)
+    _, sx, sw = lib.fp4_mx_linear_fwd(ctx, x, w, f)
+    dx, dw = lib.fp4_mx_linear_bwd(ctx, dy, sx, sw)
+    only, none = lib.fp4_mx_linear_bwd(ctx, dy, None, sw, want_dw=False)
+    assert none is None and torch.equal(only, dx)
+    none, only = lib.fp4_mx_linear_bwd(ctx, dy, sx, None, want_dx=False)
+    assert none is None and torch.equal(only, dw)
+    with pytest.raises(lib.Fp4Error):
+        lib.fp4_mx_linear_bwd(ctx, dy, sx, None)

@@ -47,3 +47,18 @@ def test_an_operand_of_another_device_is_refused_ahead_of_its_amax(ctx):
     with pytest.raises(AssertionError, match="device"):
         fp4.fp4_mx_quantize(ctx, torch.zeros(4, 64), fp4.FP4_MX_NVFP4, out=q, amax=torch.tensor([0.25]))
     assert q.struct.flags == 0 and float(q.amax) == 0.0
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="accepted calls would run on made-up addresses")
+def test_a_backward_pass_needs_only_the_operand_it_reads(lib):
+    """A frozen layer has nothing for dW.  (The stand-in of a context has no workspace, which is asked for behind all checks of operands.)"""
+    M, K, N, P, null, workspace = 8, 64, 32, 0x10000, -1, -5
+    buf = C.create_string_buffer(8192)
+    ctx, mat = C.cast(buf, C.c_void_p), lambda ld: mx.fp4_mx_matrix(P, ld, 0, 0)                  # noqa: E731
+    sx, sw = mx.fp4_mx_tensor(M, K, None, None, P, P, None, 0, 0), mx.fp4_mx_tensor(K, N, P, P, None, None, None, 0, 0)
+    ref = lambda o: None if o is None else C.byref(o)                                         # noqa: E731
+    call = lambda x, w, dx, dw: lib.fp4_mx_linear_bwd(ctx, None, ref(mat(N)), ref(x), ref(w), M, K, N, 0, ref(dx), ref(dw), P)   # noqa: E731
+    assert call(None, sw, mat(K), None) == workspace and call(sx, None, None, mat(N)) == workspace
+    assert call(None, sw, mat(K), mat(N)) == null and call(sx, None, mat(K), mat(N)) == null
+    assert call(None, sw, None, mat(N)) == null and call(sx, None, mat(K), None) == null
+    assert call(None, None, None, None) == 0
