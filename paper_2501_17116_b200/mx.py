@@ -42,12 +42,21 @@ ENTRIES = ("quantize", "dequantize", "gemm", "linear_fwd", "linear_bwd", "swiglu
 QUANTIZE, DEQUANTIZE, GEMM, LINEAR_FWD, LINEAR_BWD, SWIGLU_FWD, SWIGLU_BWD = range(7)
 
 
+class _Calls:
+    """The functions of the module _mx_call, which is loaded when the first of them is asked for: the library's other calls need no
+    part of it."""
+
+    def __getattr__(self, name: str):
+        from . import _mx_call
+        self.__dict__.update({f: getattr(_mx_call, f) for f in ENTRIES})
+        return getattr(_mx_call, name)
+
+
+_call = _Calls()
+
+
 def declare(lib: C.CDLL):
     """Prototypes of the fp4_mx_* functions, and the addresses that _mx_call takes."""
-    global _call
-    if _call is None:
-        from . import _mx_call
-        _call = _mx_call
     vp, i64, i32 = C.c_void_p, C.c_int64, C.c_int
     mat, ten = C.POINTER(fp4_mx_matrix), C.POINTER(fp4_mx_tensor)
     lib.fp4_mx_pitch.argtypes, lib.fp4_mx_pitch.restype = [i64, i32], i64
@@ -64,7 +73,6 @@ def declare(lib: C.CDLL):
 
 
 _stream_of = torch._C._cuda_getCurrentRawStream
-_call = None                               # the module _mx_call, once a library is loaded
 
 
 def _head(ctx: Context, entry: int):

@@ -62,3 +62,37 @@ def test_a_backward_pass_needs_only_the_operand_it_reads(lib):
     assert call(None, sw, mat(K), mat(N)) == null and call(sx, None, mat(K), mat(N)) == null
     assert call(None, sw, None, mat(N)) == null and call(sx, None, mat(K), None) == null
     assert call(None, None, None, None) == 0
+
+
+def fresh(code):
+    """Standard output of `code` in an interpreter of its own."""
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr
+    return done.stdout.split()
+
+
+def test_the_library_loads_without_the_module_of_the_block_scaled_calls(lib):
+    """It takes torch's headers and the interpreter's to build, and nothing else of the package needs it."""
+    assert fresh("""
+import sys
+sys.modules["paper_2501_17116_b200._mx_call"] = None                  # importing it fails
+import paper_2501_17116_b200 as fp4
+lib = fp4.load_library()
+print(lib.fp4_workspace_bytes(128, 128, 128) > 0, lib.fp4_mx_pitch(129, 0))
+try:
+    fp4.mx._call.quantize
+except ImportError:
+    print("refused")
+""") == ["True", "128", "refused"]
+
+
+def test_the_module_is_loaded_at_the_first_call_and_kept(lib):
+    assert fresh("""
+import sys
+import paper_2501_17116_b200 as fp4
+fp4.load_library()
+name = "paper_2501_17116_b200._mx_call"
+print(name in sys.modules)
+first = fp4.mx._call.gemm
+print(name in sys.modules, first is fp4.mx._call.gemm, sorted(vars(fp4.mx._call)) == sorted(fp4.mx.ENTRIES))
+""") == ["False", "True", "True", "True"]
