@@ -7,10 +7,14 @@ on the stream that is current there.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
+import os
+import sys
 
 import torch
 
 from .binding import Context, _check, _ptr, load_library
+from .build import call_path
 
 FP4_MX_E2M1 = 0
 FP4_MX_NVFP4 = 1
@@ -47,9 +51,25 @@ class _Calls:
     part of it."""
 
     def __getattr__(self, name: str):
-        from . import _mx_call
-        self.__dict__.update({f: getattr(_mx_call, f) for f in ENTRIES})
-        return getattr(_mx_call, name)
+        module = _load_call()
+        self.__dict__.update({f: getattr(module, f) for f in ENTRIES})
+        return getattr(module, name)
+
+
+def _load_call():
+    """The module of this torch and this interpreter (build.call_path); one that was built for others is not looked at."""
+    name = __package__ + "._mx_call"
+    if name not in sys.modules:
+        path = call_path()
+        if not os.path.exists(path):
+            raise ImportError(f"{path} is missing: build it with `python -m paper_2501_17116_b200.build`", name=name, path=path)
+        spec = importlib.util.spec_from_file_location(name, path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        sys.modules[name] = module
+    if sys.modules[name] is None:
+        raise ImportError(f"import of {name} halted; None in sys.modules", name=name)
+    return sys.modules[name]
 
 
 _call = _Calls()

@@ -96,3 +96,21 @@ print(name in sys.modules)
 first = fp4.mx._call.gemm
 print(name in sys.modules, first is fp4.mx._call.gemm, sorted(vars(fp4.mx._call)) == sorted(fp4.mx.ENTRIES))
 """) == ["False", "True", "True", "True"]
+
+
+def test_the_module_is_of_this_torch_and_this_interpreter(lib):
+    """One that another torch's headers were read for would misread tensors: its name is another, and it is built anew."""
+    assert os.path.exists(fp4_build.call_path()) and not fp4_build.needs_build()
+    assert fresh("""
+import torch
+from paper_2501_17116_b200 import build
+import paper_2501_17116_b200 as fp4
+fp4.load_library()
+mine = build.call_path()
+torch.__version__ = "0.0.1"
+print(build.call_path() != mine, build.needs_build())
+try:
+    fp4.mx._call.gemm
+except ImportError as e:
+    print("build" in str(e))
+""") == ["True", "True", "True"]
