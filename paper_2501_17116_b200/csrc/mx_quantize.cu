@@ -713,18 +713,21 @@ __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_con
 
 // -------------------------------------------------------------------------------- SwiGLU ---
 // h = g sigmoid(g) u in fp32, rounded once.  sigmoid(g) and 1 - sigmoid(g) = sigmoid(-g) from exp(-|g|), which cannot overflow: neither loses its
-// digits where it is small.  Two approximate instructions and a square: exp(-|g|) to 2^-21 (and 2^-25 |g| from the exponent's rounding), the
-// reciprocal to 2^-23.
+// digits where it is small.  Two approximate instructions and a square: exp(-|g|) = v^2, v = 2^(-|g| log2(e) / 2) to 2^-22, and the reciprocal to 2^-23;
+// the rounded exponent and constant add at most 1.23 |g| 2^-24 to the square.  From g = -87 on the square is below fp32's normal range, where
+// what stands beside it may be large enough for an ordinary result (g = -100, u = 3e38: 1.7 % off with the square itself).  So one
+// v goes to the small factors and the other comes last; v itself is normal down to g = -174, and from there on counts as 0.
 struct Sigmoid {
-  float s, rest;               // sigmoid(g), sigmoid(-g)
+  float part, last;            // sigmoid(g) = part last
+  float rest;                  // sigmoid(-g)
 };
 __device__ __forceinline__ Sigmoid sigmoid(float g) {
-  // exp(-|g|) as the square of 2^(-|g| log2(e) / 2), which is a normal number wherever its square is more than nothing
-  float h, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(h) : "f"(fabsf(g) * -0.7213475204444817f));
-  const float e = h * h;
+  float v, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(v) : "f"(fabsf(g) * -0.7213475204444817f));
+  const float e = v * v;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return {(g < 0.0f ? e : 1.0f) * r, (g < 0.0f ? 1.0f : e) * r};
+  const float last = g < 0.0f ? v : 1.0f;
+  return {r * last, last, (g < 0.0f ? 1.0f : e) * r};
 }
 
 struct SwigluArgs {
@@ -806,7 +809,8 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       const float g0 = g.get(2 * k), g1 = g.get(2 * k + 1);
-      g.set_pair(k, g0 * sigmoid(g0).s * u[i].get(2 * k), g1 * sigmoid(g1).s * u[i].get(2 * k + 1));
+      const Sigmoid s0 = sigmoid(g0), s1 = sigmoid(g1);
+      g.set_pair(k, g0 * s0.part * u[i].get(2 * k) * s0.last, g1 * s1.part * u[i].get(2 * k + 1) * s1.last);
     }
     if (a.has_h || a.across.on) store_run(tile, r, run, g);
     if (a.along.on) encode_along<T, FP4_MX_E2M1>(g, r, run, NO_TENSOR_SCALE, s_along, s_scale[0], bad);
@@ -881,10 +885,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_sw
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const Sigmoid s = sigmoid(g[k]);
-        const float gs = g[k] * s.s, dh = d.get(4 * q + k);
-        du[k] = dh * gs;
-        dg[k] = dh * u[k] * fmaf(gs, s.rest, s.s);         // d/dg g s = s (1 + g (1 - s)) = s + g s (1 - s)
-        hv[k] = gs * u[k];
+        const float gs = g[k] * s.part, dh = d.get(4 * q + k);
+        du[k] = dh * gs * s.last;
+        dg[k] = dh * u[k] * fmaf(gs, s.rest, s.part) * s.last;      // d/dg g s = s (1 + g (1 - s)) = s + g s (1 - s)
+        hv[k] = gs * u[k] * s.last;
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
