@@ -50,7 +50,8 @@ cudaError_t mx_allow_smem(int device, int bytes) {
 }
 
 // The kernels are launched so that one may start while the one before it on the stream drains (programmatic dependent launch): it sets
-// itself up and waits here, ahead of its first access to global memory, until everything before it is complete and visible.
+// itself up and waits here, ahead of its first access to global memory, until everything before it is complete and visible.  Global memory is read by
+// ordinary loads alone: non-coherent ones (ld.global's read-only form) promise that nothing changes while the kernel runs, and need not stay behind the wait.
 __device__ __forceinline__ void mx_wait_for_inputs() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Behind that, when the block holds all that it needs of its SM (tensor memory!): the next kernel's blocks may come, and must not get hold of
 // what a block that they wait for is still to be given.

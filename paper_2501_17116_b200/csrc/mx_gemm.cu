@@ -162,7 +162,7 @@ __device__ __forceinline__ float2 tensor_scales(uint32_t amax_a, uint32_t amax_b
   return make_float2(mx_codes::pow2_int(k / 2), mx_codes::pow2_int(k - k / 2));
 }
 __device__ __forceinline__ float2 tensor_scales(const Powers& p) {
-  return p.a ? tensor_scales(__ldg(p.a), __ldg(p.b)) : make_float2(1.0f, 1.0f);
+  return p.a ? tensor_scales(*p.a, *p.b) : make_float2(1.0f, 1.0f);
 }
 
 // 32 rows x 32 columns (the last ones: fewer) of a warp, row `lane` in y.  Ways out:
@@ -907,7 +907,7 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     const FewX& x = args.x;
     float2 tensor = make_float2(1.0f, 1.0f);
     if (FMT == FP4_MX_NVFP4) {
-      const uint32_t m = x.find ? few_amax<T>(x, s_amax + 1) : __ldg(x.amax);
+      const uint32_t m = x.find ? few_amax<T>(x, s_amax + 1) : *x.amax;
       const int k = mx_tensor_exponent(m);
       tensor = make_float2(mx_codes::pow2_int(k), mx_codes::pow2_int(-k));
       if (threadIdx.x == 64) {
@@ -939,7 +939,7 @@ mx_gemm_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (args.splits > 1) cluster_sync_all();
-  const float2 scales = MAKE && FMT == FP4_MX_NVFP4 ? tensor_scales(*s_amax, __ldg(args.powers.b)) : tensor_scales(args.powers);
+  const float2 scales = MAKE && FMT == FP4_MX_NVFP4 ? tensor_scales(*s_amax, *args.powers.b) : tensor_scales(args.powers);
   // four neighbouring columns of a token at a time, and four such fours on their way together
   constexpr int AT_ONCE = 4;
   const int step = args.splits * int(blockDim.x), n = args.out.I * (BM / 4);

@@ -468,7 +468,7 @@ __device__ __forceinline__ uint32_t thread_amax(const AmaxArgs& a, int64_t warp,
     uint4 q[AT_ONCE];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i)
-      q[i] = p + 512 * i < tail ? __ldg(reinterpret_cast<const uint4*>(p + 512 * i)) : make_uint4(0, 0, 0, 0);
+      q[i] = p + 512 * i < tail ? *reinterpret_cast<const uint4*>(p + 512 * i) : make_uint4(0, 0, 0, 0);
     const auto take = [&](uint32_t w) { m = FINITE ? most_finite<T>(m, w) : TypeOf<T>::most(m, w); };
     if (piece == 0) {                                      // up to 16 / E - 1 elements at either end
       if (begin + lane * E < body) take(element(begin + lane * E));

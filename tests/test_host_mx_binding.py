@@ -114,3 +114,16 @@ try:
 except ImportError as e:
     print("build" in str(e))
 """) == ["True", "True", "True"]
+
+
+def test_kernels_that_start_early_read_no_memory_as_constant():
+    """They are there before the kernel ahead of them has written what they read: non-coherent loads (which promise that nothing changes while the
+    kernel runs, may be served by a line from before, and may be moved ahead of the wait) have no place in them."""
+    csrc, seen = fp4_build.CSRC, 0
+    for name in sorted(os.listdir(csrc)):
+        if name.startswith("mx") and name.endswith((".cu", ".cuh")):
+            with open(os.path.join(csrc, name)) as f:
+                text = f.read()
+            seen += "mx_wait_for_inputs();" in text
+            assert not [w for w in ("__ldg", ".nc.", "__restrict__", "__ldcs") if w in text], name
+    assert seen >= 2
