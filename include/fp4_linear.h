@@ -314,9 +314,10 @@ int fp4_set_overlap(fp4_ctx* ctx, int on);
 #define FP4_QUANTILE_TOKEN  2
 int fp4_set_quantile_mode(fp4_ctx* ctx, int mode);
 /* Failure-path testing (no counterpart in the paper).  FP4_DEBUG_WAIT_LIMIT_US: the limit, in
- * microseconds, of every device-side wait of the GEMM kernels this context launches from now on
- * (0 restores the default of 2 s).  FP4_DEBUG_SKIP_FILL: the producer of the GEMM's first CTA leaves
- * out its fill number `value` of the shared-memory ring (no copy, no arrival; -1: none), so that
+ * microseconds, of every device-side wait of the GEMM and fp4_mx_* kernels this context launches from now
+ * on (0 restores the default of 2 s).  FP4_DEBUG_SKIP_FILL: the producer of the GEMM's first CTA leaves
+ * out its fill number `value` of the shared-memory ring (no copy, no arrival; -1: none; a block of
+ * fp4_mx_quantize, _dequantize and _swiglu_* has one, 0), so that
  * the consumer's wait runs out: the kernel raises FP4_DEV_TIMEOUT, frees its tensor memory and
  * returns; the context stays usable.                                                        */
 #define FP4_DEBUG_WAIT_LIMIT_US 1

@@ -14,6 +14,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "tc_ptx.cuh"
 
 constexpr int MX_TILE = 128;
 
@@ -37,6 +38,8 @@ __host__ __device__ inline int mx_tensor_exponent(uint32_t amax_bits) {
   const int k = int(((amax_bits & 0x7FFFFFFFu) + (0x7FFFFFu - 0x280000u)) >> 23) - 127 - 11;
   return k < -100 ? -100 : k;
 }
+
+inline uint64_t mx_wait_limit(const fp4_ctx* ctx) { return ctx->debug_wait_limit_ns ? ctx->debug_wait_limit_ns : WAIT_LIMIT_NS; }
 
 // More than 48 KB of shared memory for a kernel: asked for once per kernel and device (the call takes half a microsecond).
 template <auto KERNEL>

@@ -1006,7 +1006,6 @@ Powers powers_of(const MxGemm& g) {
   if (g.format != FP4_MX_NVFP4) return {nullptr, nullptr};
   return {reinterpret_cast<const uint32_t*>(g.a_amax), reinterpret_cast<const uint32_t*>(g.b_amax)};
 }
-uint64_t wait_limit(const fp4_ctx* ctx) { return ctx->debug_wait_limit_ns ? ctx->debug_wait_limit_ns : WAIT_LIMIT_NS; }
 
 // Times (ns) of the forms, as a model: a launch, then for each tile of the busiest worker a fixed part and one per k-block.  Fitted to
 // 21 sizes from 256 x 256 x 8192 to 4096 x 4096 x 4096 in all forms (within 5 % by root mean square, 16 % at worst; blocks of 16 cost a tenth
@@ -1079,7 +1078,7 @@ int launch_tiles_as(fp4_ctx* ctx, cudaStream_t stream, const MxGemm* g, int n, i
   if (args.stages > MAX_STAGES) args.stages = MAX_STAGES;
   args.idesc = idesc_mx(FMT, CTAS * BM, bn);
   args.status = status;
-  args.wait_limit_ns = wait_limit(ctx);
+  args.wait_limit_ns = mx_wait_limit(ctx);
   args.skip_fill = ctx->debug_skip_fill;
   int64_t tiles = 0;
   for (int i = 0; i < n; ++i) {
@@ -1146,7 +1145,7 @@ int launch_few(fp4_ctx* ctx, cudaStream_t stream, const MxGemm& g, int splits, i
   args.out = out_args(g);
   args.powers = powers_of(g);
   args.status = status;
-  args.wait_limit_ns = wait_limit(ctx);
+  args.wait_limit_ns = mx_wait_limit(ctx);
   args.skip_fill = ctx->debug_skip_fill;
   if (MAKE) args.x = *from;
   int rc = make_codes_map(ctx, &w, g.b, g.J, g.C, BM);

@@ -198,6 +198,16 @@ struct Loader {
   uint64_t bar;
   int abort;
 };
+__device__ __forceinline__ bool left_out(int skip_fill) { return skip_fill == 0 && blockIdx.x == 0; }
+// The tile's copies have come.  (Or did not within the limit: they are given a last millisecond, since a block must not leave ahead of its
+// copies, whose place in shared memory would be another block's by then.)
+__device__ __forceinline__ bool tile_came(Loader* l, int32_t* status, uint64_t limit_ns) {
+  if (mbar_wait(&l->bar, 0, &l->abort, status, limit_ns)) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait(&l->bar, 0))
+    if (global_timer_ns() - t0 > 1000000ull) break;
+  return false;
+}
 template <class T>
 __device__ __forceinline__ void request_tile(const Side& s, Loader* l, uint8_t* tile, int64_t row0, int64_t col0) {   // one thread
   constexpr int PER = 128 / int(sizeof(T));
@@ -542,6 +552,8 @@ struct QuantArgs {
   int parts;
   bool backwards;              // the last tile first: what the pass for the amax has left in L2
   int32_t* status;
+  uint64_t wait_limit_ns;
+  int skip_fill;               // fp4_debug_set
 };
 // One tensor or two in a launch.
 struct QuantBatch {
@@ -570,7 +582,7 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
   mx_wait_for_inputs();
   mx_let_next_start();
   if (a.x.wide) {
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
       mbar_arrive_expect_tx(&l.bar, tile_bytes<T>());
       request_tile<T>(a.x, &l, tile, row0, col0);
     }
@@ -596,7 +608,7 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
     tensor = make_float2(pow2_int(k), pow2_int(-k));
   }
   __syncthreads();
-  if (a.x.wide && !mbar_wait(&l.bar, 0, &l.abort, a.status)) return;      // (a copy that never comes: nothing is written)
+  if (a.x.wide && !tile_came(&l, a.status, a.wait_limit_ns)) return;
   bool bad = false;
   if (ROWS) {
     const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
@@ -653,6 +665,8 @@ struct DequantArgs {
   const uint32_t* amax;
   int64_t rows, cols;
   int32_t* status;
+  uint64_t wait_limit_ns;
+  int skip_fill;               // fp4_debug_set
 };
 template <class T, int FMT>
 __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_constant__ DequantArgs a) {
@@ -672,14 +686,14 @@ __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_con
   }
   mx_wait_for_inputs();
   mx_let_next_start();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
     mbar_arrive_expect_tx(&l.bar, CODE_BYTES);
     tma_load_2d(s_codes, &a.codes.map, &l.bar, int(at.col) * code_row_bytes(FMT), int(row0));
   }
   copy_scales(s_scale, a.scales + (at.row * col_tiles + at.col) * BYTES, BYTES);
   const float tensor = FMT == FP4_MX_NVFP4 ? pow2_int(mx_tensor_exponent(*a.amax)) : 1.0f;
   __syncthreads();
-  if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
+  if (!tile_came(&l, a.status, a.wait_limit_ns)) return;
   const int r = threadIdx.x & 127, run0 = (threadIdx.x >> 7) * 2;
 #pragma unroll
   for (int run = run0; run < run0 + 2; ++run) {
@@ -739,6 +753,8 @@ struct SwigluArgs {
   Codes along, across;         // h as an operand
   int64_t rows, cols;
   int32_t* status;
+  uint64_t wait_limit_ns;
+  int skip_fill;               // fp4_debug_set
 };
 // h (in `tile`, complete) as an operand and as a matrix.
 template <class T>
@@ -780,7 +796,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd
   }
   mx_wait_for_inputs();
   mx_let_next_start();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
     mbar_arrive_expect_tx(&l.bar, (a.gate.wide ? tile_bytes<T>() : 0) + (a.up.wide ? tile_bytes<T>() : 0));
     if (a.gate.wide) request_tile<T>(a.gate, &l, tile, row0, col0);
     if (a.up.wide) request_tile<T>(a.up, &l, t_up, row0, col0);
@@ -788,7 +804,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd
   if (!a.gate.wide) copy_tile_in<T>(a.gate, tile, row0, col0, a.rows, a.cols);
   if (!a.up.wide) copy_tile_in<T>(a.up, t_up, row0, col0, a.rows, a.cols);
   __syncthreads();
-  if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
+  if (!tile_came(&l, a.status, a.wait_limit_ns)) return;
   bool bad = false;
   const int r = threadIdx.x & 127, half = threadIdx.x >> 7;
   Run<T> u[2];
@@ -852,7 +868,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_sw
   }
   mx_wait_for_inputs();
   mx_let_next_start();
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
     mbar_arrive_expect_tx(&l.bar, 2 * CODES8 + (a.dh.wide ? tile_bytes<T>() : 0));
     tma_load_2d(t_up, &a.ckpt_gate.codes.map, &l.bar, int(at.col) * 128, int(row0));
     tma_load_2d(t_up + CODES8, &a.ckpt_up.codes.map, &l.bar, int(at.col) * 128, int(row0));
@@ -862,7 +878,7 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_sw
   copy_scales(s_scale[2], a.ckpt_gate.scales + (at.row * a.ckpt_gate.tiles + at.col) * 512, 512);
   copy_scales(s_scale[3], a.ckpt_up.scales + (at.row * a.ckpt_up.tiles + at.col) * 512, 512);
   __syncthreads();
-  if (!mbar_wait(&l.bar, 0, &l.abort, a.status)) return;
+  if (!tile_came(&l, a.status, a.wait_limit_ns)) return;
   bool bad = false;
   const int r = threadIdx.x & 127, half = threadIdx.x >> 7;
   Run8 cg[2], cu[2];
@@ -1077,6 +1093,8 @@ int launch_mx_quantize(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize* what
     a.cols = q[i]->cols;
     a.amax = reinterpret_cast<uint32_t*>(q[i]->amax);
     a.status = status;
+    a.wait_limit_ns = mx_wait_limit(ctx);
+    a.skip_fill = ctx->debug_skip_fill;
     batch.tiles[i] = unsigned(mx_tiles(a.rows) * mx_tiles(a.cols));
     int rc = matrix_side(ctx, &a.x, what[i].x, a.rows, a.cols, dtype, false);
     if (rc == FP4_OK) rc = codes_along(ctx, &a.along, *q[i], a.rows, a.cols);
@@ -1096,6 +1114,8 @@ int launch_mx_dequantize(fp4_ctx* ctx, cudaStream_t stream, const uint8_t* codes
   a.rows = rows;
   a.cols = cols;
   a.status = status;
+  a.wait_limit_ns = mx_wait_limit(ctx);
+  a.skip_fill = ctx->debug_skip_fill;
   int rc = codes_side(ctx, &a.codes, codes, rows, cols, format);
   if (rc == FP4_OK) rc = matrix_side(ctx, &a.out, out, rows, cols, dtype, true);
   if (rc != FP4_OK) return rc;
@@ -1112,6 +1132,8 @@ int launch_mx_swiglu_fwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix gate, MxMat
   a.rows = rows;
   a.cols = cols;
   a.status = status;
+  a.wait_limit_ns = mx_wait_limit(ctx);
+  a.skip_fill = ctx->debug_skip_fill;
   a.has_h = h.p != nullptr;
   int rc = matrix_side(ctx, &a.gate, gate, rows, cols, dtype, false);
   if (rc == FP4_OK) rc = matrix_side(ctx, &a.up, up, rows, cols, dtype, false);
@@ -1130,6 +1152,8 @@ int launch_mx_swiglu_bwd(fp4_ctx* ctx, cudaStream_t stream, MxMatrix dh, const f
   a.rows = rows;
   a.cols = cols;
   a.status = status;
+  a.wait_limit_ns = mx_wait_limit(ctx);
+  a.skip_fill = ctx->debug_skip_fill;
   a.has_h = h.p != nullptr;
   int rc = matrix_side(ctx, &a.dh, dh, rows, cols, dtype, false);
   if (rc == FP4_OK) rc = matrix_side(ctx, &a.gate, dgate, rows, cols, dtype, true);
