@@ -198,7 +198,8 @@ struct Loader {
   uint64_t bar;
   int abort;
 };
-__device__ __forceinline__ bool left_out(int skip_fill) { return skip_fill == 0 && blockIdx.x == 0; }
+// Whether the thread asks for the block's tile.  (Called ahead of the wait for the inputs: the switch is a parameter that is not in the constant cache yet.)
+__device__ __forceinline__ bool asks_for_tile(int skip_fill) { return threadIdx.x == 0 && !(skip_fill == 0 && blockIdx.x == 0); }
 // The tile's copies have come.  (Or did not within the limit: they are given a last millisecond, since a block must not leave ahead of its
 // copies, whose place in shared memory would be another block's by then.)
 __device__ __forceinline__ bool tile_came(Loader* l, int32_t* status, uint64_t limit_ns) {
@@ -579,10 +580,11 @@ __global__ void __launch_bounds__(THREADS) mx_quantize_kernel(const __grid_const
     l.abort = 0;
     fence_async_smem();
   }
+  const bool asks = asks_for_tile(a.skip_fill);
   mx_wait_for_inputs();
   mx_let_next_start();
   if (a.x.wide) {
-    if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
+    if (asks) {
       mbar_arrive_expect_tx(&l.bar, tile_bytes<T>());
       request_tile<T>(a.x, &l, tile, row0, col0);
     }
@@ -684,9 +686,10 @@ __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_con
     l.abort = 0;
     fence_async_smem();
   }
+  const bool asks = asks_for_tile(a.skip_fill);
   mx_wait_for_inputs();
   mx_let_next_start();
-  if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
+  if (asks) {
     mbar_arrive_expect_tx(&l.bar, CODE_BYTES);
     tma_load_2d(s_codes, &a.codes.map, &l.bar, int(at.col) * code_row_bytes(FMT), int(row0));
   }
@@ -794,9 +797,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 3) mx_swiglu_fwd
     l.abort = 0;
     fence_async_smem();
   }
+  const bool asks = asks_for_tile(a.skip_fill);
   mx_wait_for_inputs();
   mx_let_next_start();
-  if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
+  if (asks) {
     mbar_arrive_expect_tx(&l.bar, (a.gate.wide ? tile_bytes<T>() : 0) + (a.up.wide ? tile_bytes<T>() : 0));
     if (a.gate.wide) request_tile<T>(a.gate, &l, tile, row0, col0);
     if (a.up.wide) request_tile<T>(a.up, &l, t_up, row0, col0);
@@ -866,9 +870,10 @@ __global__ void __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : H ? 2 : 3) mx_sw
     l.abort = 0;
     fence_async_smem();
   }
+  const bool asks = asks_for_tile(a.skip_fill);
   mx_wait_for_inputs();
   mx_let_next_start();
-  if (threadIdx.x == 0 && !left_out(a.skip_fill)) {
+  if (asks) {
     mbar_arrive_expect_tx(&l.bar, 2 * CODES8 + (a.dh.wide ? tile_bytes<T>() : 0));
     tma_load_2d(t_up, &a.ckpt_gate.codes.map, &l.bar, int(at.col) * 128, int(row0));
     tma_load_2d(t_up + CODES8, &a.ckpt_up.codes.map, &l.bar, int(at.col) * 128, int(row0));
