@@ -364,13 +364,15 @@ int fp4_quantile_thresholds_static(void* stream, const void* x_bf16, int64_t row
  *
  *   FP4_MX_E2M1   E2M1 nibbles, blocks of 32, scale 2^e (E8M0 byte e + 127): e is the least integer in
  *                 [-127, 127] with amax <= 6 * 2^e, amax the block's largest magnitude (a block of zeros:
- *                 -127); code = E2M1(x * 2^-e).  ("MXFP4".)
+ *                 -127); code = E2M1(x * 2^-e).  ("MXFP4".  The OCP conversion takes floor(log2 amax) - 2
+ *                 for e and saturates; this e is one more where amax / 2^e would exceed 6, so codes and
+ *                 scales differ there.  The format, what codes and scales stand for, is the same.)
  *   FP4_MX_NVFP4  E2M1 nibbles, blocks of 16, an E4M3 scale s each and a scale g of the whole tensor: g is
  *                 the least power of two, 2^-100 at least, with the tensor's amax (its largest finite
  *                 magnitude) <= 6 * 448 * g;
  *                 s = E4M3(amax / g / 6), code = E2M1(x / g / s), 0 where s is 0.  The tensor's amax is kept
  *                 (`amax`), g follows from it.
- *   FP4_MX_E4M3   E4M3 bytes, blocks of 32, scale 2^e with amax <= 448 * 2^e: the 8-bit form in which
+ *   FP4_MX_E4M3   E4M3 bytes, blocks of 32, scale 2^e with amax <= 448 * 2^e (likewise): the 8-bit form in which
  *                 activations are kept for the backward pass.  fp4_mx_gemm does not take it.
  * E2M1() and E4M3() round to the nearest value, ties to even, and saturate (which only a given amax that is
  * too small can cause).  E2M1 codes of -0 are written as 0.  A block with an infinity or a NaN gets the

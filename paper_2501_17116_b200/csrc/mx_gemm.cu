@@ -18,9 +18,10 @@
 // memory in order of rank.  Of very few tokens it takes the values themselves (a layer's forward pass onto weights that are there): each CTA
 // quantises what its k-blocks need while the weights travel, which saves the quantiser's launch and the wait for it.
 //
-// What bounds it: at 8192^3 (177 us in blocks of 32, 190 in blocks of 16, 6.2 and 5.8 PFLOP/s; the power cap in a long run: 209) the operands' way from L2: a
+// What bounds it: at 8192^3 (173 us in blocks of 32, 181 in blocks of 16, 6.4 and 6.1 PFLOP/s; the power cap in a long run: 206) the operands' way from L2: a
 // pair's k-block of 256 x 256 is 35 KB a CTA, 60 bytes a clock at the tensor cores' rate, where L2 gives 64; a 256 x 256 x 2048 tile takes 4650 cycles alone
-// and 6000 beside 73 others.  Few rows: a launch and the weight's bytes, 1 x 4096 x 11008 7.7 us, 8 x 8192 x 28672 5.1 TB/s.
+// and 6000 beside 73 others.  Few rows: a launch and the weight's bytes; tokens x contraction x weight rows back to back, the tokens an operand already and
+// the weights from HBM: 1 x 4096 x 11008 7.8 us, 8 x 8192 x 28672 21.8 (5.7 TB/s).
 // Every wait is bounded: on a timeout a CTA raises FP4_DEV_TIMEOUT, drains its copies, frees its tensor memory and returns.
 #include <cuda.h>
 #include <cuda_fp16.h>
@@ -1007,10 +1008,11 @@ Powers powers_of(const MxGemm& g) {
   return {reinterpret_cast<const uint32_t*>(g.a_amax), reinterpret_cast<const uint32_t*>(g.b_amax)};
 }
 
-// Times (ns) of the forms, as a model: a launch, then for each tile of the busiest worker a fixed part and one per k-block.  Fitted to
-// 21 sizes from 256 x 256 x 8192 to 4096 x 4096 x 4096 in all forms (within 5 % by root mean square, 16 % at worst; blocks of 16 cost a tenth
-// more per k-block).  One thread issues a k-block's copies of scales and MMAs in 250 ns, whatever the width, so narrow tiles pay only where
-// they fill SMs that would idle: 1024^3 4.8 us by 128 x 64 against 6.4 by pairs 256 wide, 4096 x 2048 x 5504 45 against 19.5.
+// Times (ns) of the forms, as a model: a launch, then for each tile of the busiest worker a fixed part and one per k-block (blocks of 16 cost a tenth more
+// of it).  It is there to order the forms.  Over 24 sizes from 129 x 128 x 256 to 8192 x 5120 x 13824 in either kind of blocks its times are off by 15 % by
+// root mean square and 46 % at worst, while the form that it takes is the best of the seven or within 1.5 % of it in 40 of the 48 and 11 % behind at worst
+// (1024 x 1024 x 4096: 128 x 64 8.5 us, pairs 128 wide 7.7).  One thread issues a k-block's copies of scales and MMAs in 250 ns, whatever the width, so narrow
+// tiles pay only where they fill SMs that would idle: 1024^3 4.6 us by 128 x 64 against 5.7 by pairs 256 wide, 4096 x 2048 x 5504 47.8 against 19.3.
 struct TileForm {
   int bn;
   bool pair;
@@ -1045,8 +1047,9 @@ TileForm choose_form(const fp4_ctx* ctx, const MxGemm* g, int n) {
   return best;
 }
 
-// Few rows: into how many parts a cluster splits the contraction, and the time by the same kind of model.  As a rule more than four parts, or
-// more CTAs than SMs, cost more than they save (clusters of 8 do not fill the GPU: 1 x 4096 x 4096 5.0 us in 4 parts, 7.3 in 8; not split 6.8).
+// Few rows: into how many parts a cluster splits the contraction, and the time by the same kind of model.  As a rule no more than four parts, and no more
+// CTAs than SMs (24 tokens x contraction x weight rows, back to back with weights from HBM, 1 / 2 / 3 / 4 / 5 / 6 parts: 5504 x 2048 8.7 / 6.9 / 6.3 / 5.7 / 6.0 /
+// 6.2; 4096 x 4096 7.2 / 5.9 / 6.4 / 6.1 / 6.7 / 6.8; 100 tokens 8.3 / 7.8 / 7.9 / 8.2 / 10.8 / 10.9).
 struct FewForm {
   int splits;
   int64_t cost;
@@ -1056,7 +1059,9 @@ FewForm choose_few(const fp4_ctx* ctx, const MxGemm& g) {
   int64_t splits = ctx->num_sms / tiles;
   if (splits > (kbs + 1) / 2) splits = (kbs + 1) / 2;
   splits = splits < 1 ? 1 : (splits > 4 ? 4 : splits);
-  // (two CTAs an SM, where each still has a long way to go and the tokens take little room: 24 x 5120 x 13824 in blocks of 16, 6 parts 8.8 us, 3 parts 9.6)
+  // Two CTAs an SM, where each still has eight k-blocks, and the tokens take little room.  It hides latency, which pays where the weights are in L2, and
+  // fills the SMs unevenly, which costs where they come from HBM and the parts are few: 24 tokens x contraction x weight rows, us without / with it, from L2
+  // 4096 x 11008 7.2 / 6.4, 11008 x 4096 7.8 / 7.4, 13824 x 5120 9.3 / 7.9, 20000 x 1000 9.6 / 8.5; from HBM 7.8 / 8.3, 8.9 / 9.0, 10.4 / 10.5, 9.6 / 8.6.
   int64_t more = 2 * ctx->num_sms / tiles;
   if (more > kbs / 8) more = kbs / 8;
   if (more > 6) more = 6;
@@ -1194,12 +1199,13 @@ int launch_mx_linear_few(fp4_ctx* ctx, cudaStream_t stream, const MxQuantize& x,
   *done = false;
   if (g.I > FEW_X_ROWS || x.q->codes_t) return FP4_OK;
   const FewForm few = choose_few(ctx, g);
-  // A launch and its wait (1200 ns) against what every CTA does again (40 a part).  Tokens x contraction x weight rows, us, made by the kernel / by the
-  // quantiser: 1 x 4096 x 11008 8.8 / 10.1, 4 x 11008 x 4096 9.9 / 10.9 (44 parts), 6 x 4096 x 11008 9.8 / 10.1 (48), 8 x 4096 x 11008 10.5 / 9.4 (64);
-  // beside tiles, which few tokens take where the contraction is short, 8 x 1024 x 1024 4.8 / 5.5 (16), 16 x 1024 x 512 5.8 / 5.4 (32).
+  // A launch and its wait (1200 ns) against what every CTA does again (40 a part).  Tokens x contraction x weight rows, us back to back with the weights from
+  // HBM, made by the kernel / by the quantiser: 1 x 4096 x 11008 8.8 / 9.1, 4 x 11008 x 4096 9.8 / 10.8 (44 parts), 6 x 4096 x 11008 9.7 / 10.1 (48), 8 x 4096 x 11008
+  // 10.3 / 9.3 (64); beside tiles, which few tokens take where the contraction is short, 8 x 1024 x 1024 5.0 / 5.8 (16), 16 x 1024 x 512 6.0 / 5.7 (32).
   const int64_t per_cta = ((g.C + 255) / 256 + few.splits - 1) / few.splits, parts = g.I * per_cta;
   if (per_cta > FEW_X_BLOCKS || parts > FEW_X_PARTS || few.cost + 40 * parts > choose_form(ctx, &g, 1).cost + 1200) return FP4_OK;
-  // Where every CTA has to look for the amax first: 1 x 13824 x 5120 13.0 / 14.9, 1 x 4096 x 4096 7.6 / 8.5, 2 x 4096 x 11008 11.5 / 10.5.
+  // Where every CTA has to look for the amax first: 1 x 13824 x 5120 12.8 / 15.1, 1 x 4096 x 4096 7.6 / 8.6, 1 x 4096 x 11008 10.8 / 10.4; two tokens of the last,
+  // in a kernel that looked at more than one, 11.5 / 10.5.
   const bool find = nv && !(x.q->flags & FP4_MX_AMAX_GIVEN);
   if (find && g.I > 1) return FP4_OK;
   *done = true;

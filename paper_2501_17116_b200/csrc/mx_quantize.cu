@@ -16,11 +16,12 @@
 // the columns); either way it holds whole blocks and no two threads have to agree on an amax, and either access touches
 // every bank once.
 //
-// What bounds it: the bytes, one way and back (16384 x 8192 BF16 51 us = 6.6 TB/s, back 54); both ways also the instructions, 11.5 a value for blocks
-// of 32 (68 us, 92 % of the copy rate) and 15.4 for blocks of 16 (77 us, 80 % of the issue slots; the pass for the amax 43 us).  SwiGLU of 16384 x
-// 13824 with the checkpoint 275 us, backward 280, which is the copy rate; with h as an operand 288 and 352.  (A first version kept the tile in
-// registers, eight neighbours a lane, and found a block's amax by shuffles: 23 instructions for both directions, 75 % of the issue slots
-// at 40 % of the DRAM's throughput.)
+// What bounds it: the bytes, one way and back (16384 x 8192 BF16 to E2M1 51 us = 6.6 TB/s, back 55; to E4M3 59, back 65); both ways also the instructions, 11.5
+// a value for blocks of 32 (70 us, 90 % of the copy rate; E4M3 93) and 15.4 for blocks of 16 (78 us, 79 % of the issue slots; the pass for the amax 43).  Rows off
+// 16-byte boundaries: 129 us in blocks of 16 both ways, back 80, most of it shifting.  SwiGLU of the same size: forward 117 us, with the checkpoint 164
+// (the copy rate: 165), with the checkpoint and h as an operand along its rows in place of h 179 (135), both ways 206 (146); backward 168 (165), with h as an
+// operand along its columns 227 (176), both ways 403 (187), which takes 113 KB of shared memory, one block an SM.  (A first version kept the tile in registers, eight neighbours
+// a lane, and found a block's amax by shuffles: 23 instructions for both directions, 75 % of the issue slots at 40 % of the DRAM's throughput.)
 #include <cuda.h>
 #include <cuda_fp16.h>
 
