@@ -479,7 +479,7 @@ int fp4_mx_linear_bwd(fp4_ctx* ctx, void* stream, const fp4_mx_matrix* dy, const
  * SwiGLU between the gate / up and the down projection, with its inputs kept in 8 bits:
  *   h = gate * sigmoid(gate) * up        [rows x cols], fp32 arithmetic, rounded once
  * (the exponential is an approximate one: results are off by at most 2^-20 (1 + |gate| / 8) of themselves, d_gate of its
- * terms dh * u * s and dh * u * g * s * (1 - s), and by a rounding; sigmoid counts as 0 from a gate of -174 down; dh * u has to
+ * terms dh * u * s and dh * u * g * s * (1 - s), and by a rounding; sigmoid counts as 0 below a gate of -174.6; dh * u has to
  * stay inside of fp32's range).
  * Any of: `h` as a matrix; `quantized`, h (rounded to the inputs' type) as the operand of the down projection,
  * FP4_MX_E2M1, in the directions it has buffers for; ckpt_gate and ckpt_up (both or neither), FP4_MX_E4M3,

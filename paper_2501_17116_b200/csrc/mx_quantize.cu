@@ -734,7 +734,7 @@ __global__ void __launch_bounds__(THREADS) mx_dequantize_kernel(const __grid_con
 // digits where it is small.  Two approximate instructions and a square: exp(-|g|) = v^2, v = 2^(-|g| log2(e) / 2) to 2^-22, and the reciprocal to 2^-23;
 // the rounded exponent and constant add at most 1.23 |g| 2^-24 to the square.  From g = -87 on the square is below fp32's normal range, where
 // what stands beside it may be large enough for an ordinary result (g = -100, u = 3e38: 1.7 % off with the square itself).  So one
-// v goes to the small factors and the other comes last; v itself is normal down to g = -174, and from there on counts as 0.
+// v goes to the small factors and the other comes last; v itself is normal down to g = -174.6, and below that counts as 0.
 struct Sigmoid {
   float part, last;            // sigmoid(g) = part last
   float rest;                  // sigmoid(-g)
